@@ -71,7 +71,9 @@ typedef enum kan_status {
 typedef enum kan_dtype {
   KAN_F32 = 0, KAN_F16 = 1, KAN_I8 = 2, KAN_U16 = 3, KAN_U32 = 4,
   KAN_Q8 = 5,  /* gain and bias as one byte each: logarithmic gain code, linear bias code */
-  KAN_BFP8 = 6 /* codebook rows in block floating point, 8-bit mantissas: see kan_vq_layer  */
+  KAN_BFP8 = 6, /* codebook rows in block floating point, 8-bit mantissas: see kan_vq_layer  */
+  KAN_BF16 = 7, /* bfloat16, and 64-bit signed ids: the operators around the blocks of a      */
+  KAN_I64 = 8   /* language model only (kan_lookup_*, kan_block_norm_*, kan_vocab_loss_*)     */
 } kan_dtype;
 
 /* Which arithmetic carries the edge evaluation.
@@ -314,6 +316,82 @@ kan_status kan_vq_reconstruction_sums(const float* coef, int32_t in, int32_t out
                                       int32_t K, int32_t idx_dtype, const void* idx, const float* gain,
                                       const float* bias, double* sums, void* ws, size_t ws_bytes,
                                       void* stream);
+
+/* ---- Around the KAN blocks of a language model ----------------------------------------------------------------------
+ *
+ * Three operators, each with its gradient: what turns tokens into the input of a block, what joins a block to the residual
+ * stream, and what the model is scored and trained on.  The conventions above hold: device pointers of the caller, no
+ * allocation, no synchronisation, host validation first, work on `stream`, no state between calls; a call may be captured
+ * into a graph.  Element types: KAN_F32, KAN_F16 or KAN_BF16; arrays are row-major, contiguous and aligned to their element
+ * size.  Sums, norms and softmax statistics are fp32.  Results do not depend on timing: equal calls give equal bits.
+ * N == 0 enqueues nothing but what the sums over no tokens ask for (zeros).
+ *
+ * Ids and targets are KAN_U16 (tables of up to 65536 rows), KAN_U32 or KAN_I64; an id that is negative (KAN_I64) or not
+ * below the number of rows names no row: KAN_U32 0xffffffff, the 32-bit pattern of -1, among them.  No id is an error.     */
+
+/* Rows of a table by id, times a scale:  y[n][:] = scale * table[ids[n]][:],  zeros for an id that names no row.
+ * table [V][D], ids [N], y [N][D] (any of the three types, rounded once); D <= 2^20.                                        */
+kan_status kan_lookup_forward(const void* table, int32_t table_dtype, int32_t V, int32_t D, const void* ids, int32_t id_dtype,
+                              int64_t N, float scale, void* y, int32_t y_dtype, void* stream);
+
+/* Gradient of the table:  dtable[v][:] = scale * sum over the n with ids[n] = v, in order, of dy[n][:]  (zeros for a row that
+ * no id names), or added onto what dtable holds when accumulate is 1 (rows that no id names are then left alone).
+ * The tokens are sorted by id on the way; N <= 2^30.  With the ids of kan_vq_assign and D = 10 this is the gradient
+ * of a codebook.  dy [N][D], dtable [V][D]; dtable must not overlap dy.                                                     */
+size_t kan_lookup_backward_workspace_bytes(int32_t V, int32_t D, int64_t N);
+kan_status kan_lookup_backward(const void* dy, int32_t dy_dtype, const void* ids, int32_t id_dtype, int64_t N, int32_t V,
+                               int32_t D, float scale, void* dtable, int32_t dtable_dtype, int32_t accumulate, void* ws,
+                               size_t ws_bytes, void* stream);
+
+/* Norms around a block: host struct, device pointers. */
+typedef struct kan_block_norm {
+  int32_t D;             /* columns, 1 .. 16384                                                                  */
+  int32_t stream_dtype;  /* the residual stream: x, y, dy, dx                                                    */
+  int32_t block_dtype;   /* the blocks' inputs, outputs and gates: u, v, gate and their gradients; the stream's  */
+                         /* type or KAN_F32 (KAN blocks take and give fp32)                                      */
+  int32_t weight_dtype;  /* w_before, w_after and their gradients                                                */
+  const void* w_before;  /* [D], or NULL: all ones                                                               */
+  const void* w_after;   /* [D], or NULL: all ones                                                               */
+  float scale;           /* of the residual branch                                                               */
+  float eps;             /* > 0                                                                                  */
+} kan_block_norm;
+
+/* y = x + scale * sigma(gate) * w_after * v / sqrt(mean(v^2) + eps)     behind a block (v: its output)
+ * u = w_before * y / sqrt(mean(y^2) + eps)                              in front of the next one (u: its input)
+ * in one pass over rows x [N][D].  v == NULL: no block in front (y = x is not written; y and gate must be NULL).
+ * gate == NULL: 1 in place of sigma(gate).  u == NULL: no norm behind.  Not both v and u NULL.  y may be x.
+ * u is formed from y before its rounding.  (KAN layers clamp their inputs to [-1, 1]: w_before puts them there.)            */
+kan_status kan_block_norm_forward(const kan_block_norm* b, const void* x, const void* v, const void* gate, int64_t N, void* y,
+                                  void* u, void* stream);
+
+/* Gradients of both formulas at y (what the forward pass wrote, x where there was no block), v and gate, from the gradients
+ * dy (of y as the rest of the stream uses it; NULL: none) and du (of u; NULL: no norm behind):
+ *   dx [N][D] of the stream in front of the block, dv and dgate [N][D] of the block's output and gate (v, gate NULL: NULL),
+ *   dw_before, dw_after [D], sums over the rows (NULL: not asked for; w_before NULL or du NULL: must be NULL, w_after and v
+ *   likewise).  Not both dy and du NULL.  dx may be dy.                                                                      */
+size_t kan_block_norm_backward_workspace_bytes(const kan_block_norm* b, int64_t N);
+kan_status kan_block_norm_backward(const kan_block_norm* b, const void* y, const void* dy, const void* du, const void* v,
+                                   const void* gate, int64_t N, void* dx, void* dv, void* dgate, void* dw_before,
+                                   void* dw_after, void* ws, size_t ws_bytes, void* stream);
+
+/* Softmax cross entropy of rows h [N][D] against a table [V][D] of outputs, both of `dtype`, without the logits:
+ *   z[n][v] = scale * <h[n], table[v]>,   lse[n] = log sum_v exp z[n][v],   loss[n] = lse[n] - z[n][targets[n]]
+ * loss[n] = 0 where the target names no row (padding, masked prompts).  loss, lse: fp32 [N].  N <= 2^24, D <= 2^20.
+ * 16-bit rows whose width is a multiple of 8 must be 16-byte aligned, else KAN_ERR_SHAPE.  fp32 rows: products of fp32 grade,
+ * on values below 3.3e38 in magnitude.                                                                                      */
+size_t kan_vocab_loss_workspace_bytes(int64_t N, int32_t V, int32_t D, int32_t dtype, int32_t backward);
+kan_status kan_vocab_loss_forward(const void* h, const void* table, int32_t dtype, int64_t N, int32_t V, int32_t D,
+                                  const void* targets, int32_t id_dtype, float scale, float* loss, float* lse, void* ws,
+                                  size_t ws_bytes, void* stream);
+
+/* Gradients for the losses' gradients dloss [N] (fp32), with the lse of the forward call:
+ *   g[n][v] = scale * dloss[n] * (exp(z[n][v] - lse[n]) - [v == targets[n]]),   dh = g table,   dtable = g^t h
+ * dh [N][D], dtable [V][D] in `dtype`; accumulate 1: added onto what dtable holds (a table that is looked up as well).  A row
+ * whose target names no row has no gradient and no part in dtable, whatever h, lse and dloss hold there.  The table is dealt
+ * with in pieces, of which the workspace holds g.  dh and dtable must not overlap h or table.                                */
+kan_status kan_vocab_loss_backward(const void* h, const void* table, int32_t dtype, int64_t N, int32_t V, int32_t D,
+                                   const void* targets, int32_t id_dtype, float scale, const float* lse, const float* dloss,
+                                   void* dh, void* dtable, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
 
 /* Per-kernel timing with HIP events on the launch stream, for benchmarks.
  * kan_prof_begin creates up to max_launches event pairs (this is the one place

@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libkan_mi355x.so")
 
 KAN_OK = 0
 KAN_ERR_NULL, KAN_ERR_SHAPE, KAN_ERR_DTYPE, KAN_ERR_WORKSPACE, KAN_ERR_UNSUPPORTED, KAN_ERR_LAUNCH = 1, 2, 3, 4, 5, 6
-KAN_F32, KAN_F16, KAN_I8, KAN_U16, KAN_U32, KAN_Q8, KAN_BFP8 = 0, 1, 2, 3, 4, 5, 6
+KAN_F32, KAN_F16, KAN_I8, KAN_U16, KAN_U32, KAN_Q8, KAN_BFP8, KAN_BF16, KAN_I64 = 0, 1, 2, 3, 4, 5, 6, 7, 8
 KAN_PATH_AUTO, KAN_PATH_GATHER, KAN_PATH_MFMA = 0, 1, 2
 KAN_RULE_BSPLINE3, KAN_RULE_PLI2 = 0, 1
 
@@ -31,6 +31,9 @@ EXPORTS = [
     "kan_status_string", "kan_vq_planned_kernel", "kan_dense_planned_kernel", "kan_vq_prepared_bytes", "kan_vq_prepare", "kan_pli_basis",
     "kan_vq_assign_workspace_bytes", "kan_vq_assign_fast_workspace_bytes", "kan_vq_assign", "kan_vq_reconstruction_workspace_bytes",
     "kan_vq_reconstruction_sums", "kan_basis_window", "kan_vq_coef_range", "kan_vq_head_forward_static",
+    "kan_lookup_forward", "kan_lookup_backward_workspace_bytes", "kan_lookup_backward",
+    "kan_block_norm_forward", "kan_block_norm_backward_workspace_bytes", "kan_block_norm_backward",
+    "kan_vocab_loss_workspace_bytes", "kan_vocab_loss_forward", "kan_vocab_loss_backward",
 ]
 KAN_LAYER_NO_COLUMN = 1
 KAN_STATIC_SCRATCH_BYTES = 32 * 1024 * 1024
@@ -43,6 +46,13 @@ class kan_vq_layer(C.Structure):
         ("idx", C.c_void_p), ("gain", C.c_void_p), ("bias", C.c_void_p), ("codebook", C.c_void_p),
         ("scale", C.c_float), ("rule", C.c_int32), ("prepared", C.c_void_p),
         ("gain_log2_lo", C.c_float), ("gain_log2_step", C.c_float), ("bias_scale", C.c_float), ("flags", C.c_int32),
+    ]
+
+
+class kan_block_norm(C.Structure):
+    _fields_ = [
+        ("D", C.c_int32), ("stream_dtype", C.c_int32), ("block_dtype", C.c_int32), ("weight_dtype", C.c_int32),
+        ("w_before", C.c_void_p), ("w_after", C.c_void_p), ("scale", C.c_float), ("eps", C.c_float),
     ]
 
 
@@ -135,6 +145,25 @@ def lib():
         L.kan_vq_reconstruction_workspace_bytes.restype = SZ
         L.kan_vq_reconstruction_sums.argtypes = [P, I32, I32, P, I32, I32, P, P, P, P, P, SZ, P]
         L.kan_vq_reconstruction_sums.restype = I32
+        F, NP = C.c_float, C.POINTER(kan_block_norm)
+        L.kan_lookup_forward.argtypes = [P, I32, I32, I32, P, I32, I64, F, P, I32, P]
+        L.kan_lookup_forward.restype = I32
+        L.kan_lookup_backward_workspace_bytes.argtypes = [I32, I32, I64]
+        L.kan_lookup_backward_workspace_bytes.restype = SZ
+        L.kan_lookup_backward.argtypes = [P, I32, P, I32, I64, I32, I32, F, P, I32, I32, P, SZ, P]
+        L.kan_lookup_backward.restype = I32
+        L.kan_block_norm_forward.argtypes = [NP, P, P, P, I64, P, P, P]
+        L.kan_block_norm_forward.restype = I32
+        L.kan_block_norm_backward_workspace_bytes.argtypes = [NP, I64]
+        L.kan_block_norm_backward_workspace_bytes.restype = SZ
+        L.kan_block_norm_backward.argtypes = [NP, P, P, P, P, P, I64, P, P, P, P, P, P, SZ, P]
+        L.kan_block_norm_backward.restype = I32
+        L.kan_vocab_loss_workspace_bytes.argtypes = [I64, I32, I32, I32, I32]
+        L.kan_vocab_loss_workspace_bytes.restype = SZ
+        L.kan_vocab_loss_forward.argtypes = [P, P, I32, I64, I32, I32, P, I32, F, P, P, P, SZ, P]
+        L.kan_vocab_loss_forward.restype = I32
+        L.kan_vocab_loss_backward.argtypes = [P, P, I32, I64, I32, I32, P, I32, F, P, P, P, P, I32, P, SZ, P]
+        L.kan_vocab_loss_backward.restype = I32
         _lib = L
     return _lib
 
@@ -390,6 +419,49 @@ def kan_vq_reconstruction_r2(coef, codebook, idx, gain, bias) -> float:
                                           _ptr(bias), _ptr(sums), _ptr(ws), ws.numel(), _stream_ptr())
     _check(st, "kan_vq_reconstruction_sums")
     return float(sums[3].item())
+
+
+# ---- around the KAN blocks of a language model --------------------------------------------------------------------
+# Tensors are contiguous, of float32, float16 or bfloat16, and on the current device; ids and targets are int16 (carrying
+# uint16), int32 or int64, of any shape.  None of these calls records anything for autograd.
+
+
+def kan_lookup_forward(table, ids, scale=1.0, dtype=None, y=None):
+    """Rows of table [V][D] by id, times scale -> y [shape of ids][D] of dtype (the table's; y's when y is given).
+    An id that names no row (-1, say) gives zeros."""
+    return _done(_host().lookup_forward(table, ids, scale, dtype, y), "kan_lookup_forward")
+
+
+def kan_lookup_backward(dy, ids, rows, scale=1.0, dtype=None, dtable=None, accumulate=False, ws=None):
+    """Gradient of a table of `rows` rows from dy [shape of ids][D]: the sum of scale * dy over the tokens of each id ->
+    dtable [rows][D] of dtype (dy's), added onto the given dtable with accumulate."""
+    return _done(_host().lookup_backward(dy, ids, rows, scale, dtype, dtable, accumulate, ws), "kan_lookup_backward")
+
+
+def kan_block_norm_forward(x, v=None, gate=None, w_after=None, w_before=None, scale=1.0, eps=1e-6, dtype=None, want_u=True,
+                           y=None, u=None):
+    """y = x + scale * sigmoid(gate) * w_after * v / rms(v) and u = w_before * y / rms(y) -> (y, u), in rows of the last
+    dimension.  v is the output of the block behind which the call stands: without one y is None (the stream is x), and u
+    is the first block's input.  want_u False: no block follows, u is None.  dtype of u, v and gate: v's; x's when there is no v."""
+    return _done(_host().block_norm_forward(x, v, gate, w_after, w_before, scale, eps, dtype, want_u, y, u), "kan_block_norm_forward")
+
+
+def kan_block_norm_backward(y, dy=None, du=None, v=None, gate=None, w_after=None, w_before=None, scale=1.0, eps=1e-6, ws=None):
+    """Gradients of kan_block_norm_forward at its y (x where there was no v) from those of y and u ->
+    (dx, dv, dgate, dw_before, dw_after); None for what the call had no operand for."""
+    return _done(_host().block_norm_backward(y, dy, du, v, gate, w_after, w_before, scale, eps, ws), "kan_block_norm_backward")
+
+
+def kan_vocab_loss_forward(h, table, targets, scale=1.0, loss=None, lse=None, ws=None):
+    """Softmax cross entropy of rows h [...][D] against table [V][D] -> (loss, lse), float32 of the targets' shape.
+    loss is 0 where the target names no row (-1, say)."""
+    return _done(_host().vocab_loss_forward(h, table, targets, scale, loss, lse, ws), "kan_vocab_loss_forward")
+
+
+def kan_vocab_loss_backward(h, table, targets, lse, dloss, scale=1.0, dh=None, dtable=None, accumulate=False, ws=None):
+    """Gradients of h and table for the losses' gradients dloss (float32) -> (dh, dtable), dtable added onto the given one
+    with accumulate."""
+    return _done(_host().vocab_loss_backward(h, table, targets, lse, dloss, scale, dh, dtable, accumulate, ws), "kan_vocab_loss_backward")
 
 
 def kan_vq_planned_kernel(layer: VQLayer, B, n_heads=1, path=KAN_PATH_AUTO) -> str:

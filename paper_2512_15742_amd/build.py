@@ -48,6 +48,10 @@ UNITS = [
     ("kan_assign.hip", "kan_assign.o", []),
     ("kan_gather.hip", "kan_gather.o", []),
     ("kan_dense.hip", "kan_dense.o", []),
+    ("kan_tokens_api.hip", "kan_tokens_api.o", []),
+    ("kan_lookup.hip", "kan_lookup.o", []),
+    ("kan_norm.hip", "kan_norm.o", []),
+    ("kan_vocab.hip", "kan_vocab.o", []),
 ]
 
 

@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "kan_internal.hpp"
+#include "kan_tokens.hpp"
 
 // Scratch memory of kan_vq_head_forward_static: one array per GPU, held from the moment the
 // library's code is loaded on that GPU until the process ends.  In host code this name is only
@@ -1367,6 +1368,11 @@ kan_status plan_head(const kan_vq_layer* layers, int32_t n_layers, int32_t n_hea
 }
 
 }  // namespace
+
+kan_status run_launch(const char* name, hipStream_t s, hipError_t (*f)(const void*), const void* args) {
+  return run(name, s, [&] { return f(args); });
+}
+
 }  // namespace kan
 
 using namespace kan;

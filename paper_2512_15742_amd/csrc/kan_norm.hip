@@ -1,0 +1,341 @@
+// The norm in front of a block and the norm behind it, with gate and residual scale, in one pass over the residual stream.
+//
+//   y = x + scale * sigma(gate) * w_after * v * rv,   rv = 1 / sqrt(mean(v^2) + eps)     (v: the block's output)
+//   u = w_before * y * ry,                            ry = 1 / sqrt(mean(y^2) + eps)     (u: the next block's input)
+//
+// Backward, from y, v, gate and the gradients dy, du (t = du w_before, m = v rv, s = sigma(gate)):
+//   gy = dy + ry (t - y ry mean(t y ry))                       = dx, the gradient of the stream in front of the block
+//   q  = scale s gy w_after,   dv = rv (q - m mean(q m)),   dgate = scale gy w_after m s (1 - s)
+//   dw_before = sum du y ry,   dw_after = sum scale s gy m     (over the tokens)
+//
+// Bound by the bytes of the rows: each is read once, a row stays in the registers of one to sixteen waves, eight columns a
+// lane at a time.  Norms, means and the sums of the weights' gradients are fp32.  The u of the forward pass is formed from
+// the fp32 y, not from its rounded copy.  Backward: up to 512 groups of waves take rows in turn and keep the sums of their
+// rows' weight gradients in registers; a second launch adds the groups' sums in a fixed order.
+#include <algorithm>
+#include <type_traits>
+
+#include "kan_tokens.hpp"
+
+namespace kan {
+namespace {
+
+constexpr int kMaxGroups = 512;         // groups of waves of a backward launch, each with a partial sum of the weights' gradients
+constexpr int kMaxBlocks = 1 << 20;     // workgroups of a forward launch: they take rows in turn
+constexpr int kReduceThreads = 1024;    // 64 columns, 16 shares of the groups
+
+__device__ __forceinline__ void load_weight(const void* w, int dtype, int c, int D, float (&out)[8]) {
+  if (!w) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] = 1.f;
+  } else if (dtype == KAN_F32) {
+    load_cols((const float*)w, c, D, out);
+  } else if (dtype == KAN_F16) {
+    load_cols((const f16*)w, c, D, out);
+  } else {
+    load_cols((const bf16*)w, c, D, out);
+  }
+}
+
+// Sums of K values over the W waves of a row, the same in every lane.
+template <int W, int K>
+__device__ __forceinline__ void row_sums(float (&v)[K], float (*scratch)[K]) {
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v[k] += __shfl_xor(v[k], d);
+  if constexpr (W > 1) {
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();                 // (the scratch of the row before has been read)
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int k = 0; k < K; ++k) scratch[wave][k] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) s += scratch[w][k];
+      v[k] = s;
+    }
+  }
+}
+
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+
+// W waves a row, W == 1: four rows a workgroup.
+template <class S, class B, int W, int P>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_kernel(const NormArgs a) {
+  __shared__ float sSum[W][1];
+  const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const int D = a.D;
+  const float inv = 1.f / (float)D;
+  const long long rows = (long long)gridDim.x * (W == 1 ? 4 : 1);
+  for (long long n = W == 1 ? (long long)blockIdx.x * 4 + (threadIdx.x >> 6) : (long long)blockIdx.x; n < a.N; n += rows) {
+    float x[P][8], v[P][8], g[P][8], w[P][8];
+  #pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = (p * 64 * W + t) * 8;
+  #pragma unroll
+      for (int i = 0; i < 8; ++i) x[p][i] = v[p][i] = g[p][i] = 0.f;
+      if (c < D) {
+        load_cols((const S*)a.x + n * D, c, D, x[p]);
+        if (a.v) {
+          load_cols((const B*)a.v + n * D, c, D, v[p]);
+          if (a.gate) load_cols((const B*)a.gate + n * D, c, D, g[p]);
+          load_weight(a.w_after, a.weight_dtype, c, D, w[p]);
+        }
+      }
+    }
+    if (a.v) {
+      float ss[1] = {0.f};
+  #pragma unroll
+      for (int p = 0; p < P; ++p)
+  #pragma unroll
+        for (int i = 0; i < 8; ++i) ss[0] += v[p][i] * v[p][i];
+      row_sums<W, 1>(ss, sSum);
+      const float r = a.scale * rsqrtf(ss[0] * inv + a.eps);
+  #pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const int c = (p * 64 * W + t) * 8;
+        if (c < D) {
+  #pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float s = a.gate ? sigmoid(g[p][i]) : 1.f;
+            x[p][i] += s * (w[p][i] * (v[p][i] * r));
+          }
+          store_cols((S*)a.y + n * D, c, D, x[p]);
+          if (c + 8 > D)
+  #pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (c + i >= D) x[p][i] = 0.f;
+        }
+      }
+    }
+    if (a.u) {
+      float ss[1] = {0.f};
+  #pragma unroll
+      for (int p = 0; p < P; ++p)
+  #pragma unroll
+        for (int i = 0; i < 8; ++i) ss[0] += x[p][i] * x[p][i];
+      row_sums<W, 1>(ss, sSum);
+      const float r = rsqrtf(ss[0] * inv + a.eps);
+  #pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const int c = (p * 64 * W + t) * 8;
+        if (c < D) {
+          load_weight(a.w_before, a.weight_dtype, c, D, w[p]);
+  #pragma unroll
+          for (int i = 0; i < 8; ++i) x[p][i] = w[p][i] * (x[p][i] * r);
+          store_cols((B*)a.u + n * D, c, D, x[p]);
+        }
+      }
+    }
+  }
+}
+
+template <class S, class B, int W, int P>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_grad_kernel(const NormArgs a, int groups) {
+  __shared__ float sSum[W][3];
+  __shared__ float sSum1[W][1];
+  const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const int group = W == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  if (group >= groups) return;
+  const int D = a.D;
+  const float inv = 1.f / (float)D;
+  float sum1[P][8], sum2[P][8];
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum1[p][i] = sum2[p][i] = 0.f;
+  for (long long n = group; n < a.N; n += groups) {
+    float y[P][8], gy[P][8], du[P][8], v[P][8], g[P][8];
+    float ss[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = (p * 64 * W + t) * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[p][i] = gy[p][i] = du[p][i] = v[p][i] = g[p][i] = 0.f;
+      if (c < D) {
+        if (a.du) {
+          load_cols((const S*)a.x + n * D, c, D, y[p]);
+          load_cols((const B*)a.du + n * D, c, D, du[p]);
+        }
+        if (a.dy) load_cols((const S*)a.dy + n * D, c, D, gy[p]);
+        if (a.v) {
+          load_cols((const B*)a.v + n * D, c, D, v[p]);
+          if (a.gate) load_cols((const B*)a.gate + n * D, c, D, g[p]);
+        }
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = (p * 64 * W + t) * 8;
+      if (c < D) {
+        float w[8];
+        load_weight(a.w_before, a.weight_dtype, c, D, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          ss[0] += y[p][i] * y[p][i];
+          ss[1] += c + i < D ? du[p][i] * w[i] * y[p][i] : 0.f;
+          ss[2] += v[p][i] * v[p][i];
+        }
+      }
+    }
+    row_sums<W, 3>(ss, sSum);
+    const float ry = rsqrtf(ss[0] * inv + a.eps), rv = rsqrtf(ss[2] * inv + a.eps), mean = ss[1] * ry * inv;
+    float sq[1] = {0.f};
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = (p * 64 * W + t) * 8;
+      if (c < D) {
+        float w[8];
+        if (a.du) {
+          load_weight(a.w_before, a.weight_dtype, c, D, w);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float hat = y[p][i] * ry;
+            sum1[p][i] += du[p][i] * hat;
+            gy[p][i] += ry * (du[p][i] * w[i] - hat * mean);
+          }
+        }
+        store_cols((S*)a.dx + n * D, c, D, gy[p]);
+        if (a.v) {
+          load_weight(a.w_after, a.weight_dtype, c, D, w);
+          float dg[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float s = a.gate ? sigmoid(g[p][i]) : 1.f, m = v[p][i] * rv, e = a.scale * gy[p][i];
+            sum2[p][i] += s * e * m;
+            dg[i] = e * (w[i] * m) * (s * (1.f - s));
+            gy[p][i] = s * e * w[i];                       // q from here on
+            sq[0] += c + i < D ? gy[p][i] * m : 0.f;
+          }
+          if (a.gate) store_cols((B*)a.dgate + n * D, c, D, dg);
+        }
+      }
+    }
+    if (a.v) {
+      row_sums<W, 1>(sq, sSum1);
+      const float qm = sq[0] * inv;
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const int c = (p * 64 * W + t) * 8;
+        if (c < D) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) gy[p][i] = rv * (gy[p][i] - v[p][i] * rv * qm);
+          store_cols((B*)a.dv + n * D, c, D, gy[p]);
+        }
+      }
+    }
+  }
+  // sums[0]: w_before, then w_after, as far as they are asked for
+  float* dst = a.partial + (long long)group * D;
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int c = (p * 64 * W + t) * 8;
+    if (c < D) {
+      if (a.dw_before) store_cols(dst, c, D, sum1[p]);
+      if (a.dw_after) store_cols(dst + (a.dw_before ? (long long)groups * D : 0), c, D, sum2[p]);
+    }
+  }
+}
+
+__global__ __launch_bounds__(kReduceThreads) void kan_norm_reduce_kernel(const float* __restrict__ partial, int groups, int D, void* first, void* second,
+                                                                         int dtype) {
+  __shared__ float sSum[16][64];
+  const int lane = threadIdx.x & 63, share = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  const float* const src = partial + (long long)blockIdx.y * groups * D;
+  float s = 0.f;
+  if (c < D) {
+    int r = share;
+    for (; r + 7 * 16 < groups; r += 8 * 16) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = src[(long long)(r + u * 16) * D + c];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += v[u];
+    }
+    for (; r < groups; r += 16) s += src[(long long)r * D + c];
+  }
+  sSum[share][lane] = s;
+  __syncthreads();
+  if (share == 0 && c < D) {
+    s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s += sSum[k][lane];
+    void* const out = blockIdx.y == 0 ? first : second;
+    if (dtype == KAN_F32) ((float*)out)[c] = s;
+    else if (dtype == KAN_F16) ((f16*)out)[c] = (f16)s;
+    else ((bf16*)out)[c] = (bf16)s;
+  }
+}
+
+// f(W, P): waves per row and groups of eight columns a lane.
+template <class F>
+hipError_t with_shape(int D, F&& f) {
+#define KAN_SHAPE(W, P) if (D <= 512 * W * P) return f(std::integral_constant<int, W>{}, std::integral_constant<int, P>{})
+  KAN_SHAPE(1, 1);
+  KAN_SHAPE(1, 2);
+  KAN_SHAPE(4, 1);
+  KAN_SHAPE(4, 2);
+  KAN_SHAPE(8, 2);
+  return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
+#undef KAN_SHAPE
+}
+
+// f(S{}, B{}): the block's type is the stream's, or fp32.
+template <class F>
+hipError_t with_types(int stream, int block, F&& f) {
+  return with_float(stream, [&](auto s) {
+    if (block == stream) return f(s, s);
+    return f(s, float{});
+  });
+}
+
+int grad_groups(long long N) { return (int)std::min((long long)kMaxGroups, N); }
+
+}  // namespace
+
+hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
+  return with_types(a.stream_dtype, a.block_dtype, [&](auto st, auto bl) {
+    typedef decltype(st) S;
+    typedef decltype(bl) B;
+    return with_shape(a.D, [&](auto w, auto p) {
+      constexpr int W = decltype(w)::value, P = decltype(p)::value;
+      const long long blocks = std::min(W == 1 ? (a.N + 3) / 4 : a.N, (long long)kMaxBlocks);
+      hipLaunchKernelGGL((kan_norm_kernel<S, B, W, P>), dim3((unsigned)blocks), dim3(W == 1 ? 256 : 64 * W), 0, s, a);
+      return hipGetLastError();
+    });
+  });
+}
+
+size_t norm_grad_workspace(int D, long long N, int sums) {
+  return ((size_t)sums * grad_groups(N) * D * 4 + 255) / 256 * 256;
+}
+
+kan_status run_norm_grad(const NormArgs& a, hipStream_t s) {
+  const int groups = grad_groups(a.N);
+  kan_status st = KAN_OK;
+  if (groups > 0) st = run_named("kan_norm_grad", s, [&] {
+    return with_types(a.stream_dtype, a.block_dtype, [&](auto str, auto bl) {
+      typedef decltype(str) S;
+      typedef decltype(bl) B;
+      return with_shape(a.D, [&](auto w, auto p) {
+        constexpr int W = decltype(w)::value, P = decltype(p)::value;
+        const int blocks = W == 1 ? (groups + 3) / 4 : groups;
+        hipLaunchKernelGGL((kan_norm_grad_kernel<S, B, W, P>), dim3(blocks), dim3(W == 1 ? 256 : 64 * W), 0, s, a, groups);
+        return hipGetLastError();
+      });
+    });
+  });
+  const int sums = (a.dw_before ? 1 : 0) + (a.dw_after ? 1 : 0);
+  if (st != KAN_OK || sums == 0) return st;
+  return run_named("kan_norm_reduce", s, [&] {
+    hipLaunchKernelGGL(kan_norm_reduce_kernel, dim3((a.D + 63) / 64, sums), dim3(kReduceThreads), 0, s, a.partial, groups, a.D,
+                       a.dw_before ? a.dw_before : a.dw_after, a.dw_after, a.weight_dtype);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace kan
