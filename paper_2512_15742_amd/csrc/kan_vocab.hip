@@ -24,28 +24,29 @@ namespace {
 
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kTile = 128;              // outputs of a workgroup in either direction
 constexpr int kThreads = 256;
 constexpr int kStep = 32;               // products along the contraction per step
-constexpr int kPad = 8;
+constexpr int kTile = 256;              // results of a workgroup in either direction
+constexpr int kSlots = 4;               // steps whose operands LDS holds
 constexpr int kVocabStep = 256;         // pieces of the table are multiples of it
 constexpr long long kPackBytes = 256ll << 20, kPieceBytes = 512ll << 20;
 
-constexpr int kMaxParts = 3;
 constexpr float kHalfScale = 16384.f;   // of fp16 dS
 
 template <class T>
-__device__ __forceinline__ f32x4 mfma(uint4 a, uint4 b, f32x4 c) {
+__device__ __forceinline__ f32x16 mfma(uint4 a, uint4 b, f32x16 c) {
   if constexpr (std::is_same<T, f16>::value)
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   else
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
 // An operand of a product out[n][m] = sum_k A(m, k) B(n, k): element (r, k) at p[r * stride + k], or at p[k * stride + r];
-// rows and k of it that exist.  Parts lie `part` elements apart.
+// the rows and k of it that exist (k contiguous: a multiple of 8).  Parts lie `part` elements apart.
 struct Operand {
   const void* p;
   long long stride, part;
@@ -76,131 +77,330 @@ struct ProductArgs {
   const float* factor;       // null, or what the sums are multiplied with
 };
 
-// Which parts of A and B the products of three parts each take, the smallest first.
-__device__ constexpr int kPartA[6] = {2, 1, 0, 1, 0, 0}, kPartB[6] = {0, 1, 2, 0, 1, 0};
-
 __device__ __forceinline__ void store_any(void* p, int dtype, long long at, float v, bool add) {
   if (dtype == KAN_F32) ((float*)p)[at] = add ? ((float*)p)[at] + v : v;
   else if (dtype == KAN_F16) ((f16*)p)[at] = (f16)(add ? (float)((f16*)p)[at] + v : v);
   else ((bf16*)p)[at] = (bf16)(add ? (float)((bf16*)p)[at] + v : v);
 }
 
-// T: type of the 16-bit operands; AK, BK: their k is contiguous.
-template <class T, bool AK, bool BK, int EPI>
-__global__ __launch_bounds__(kThreads) void kan_vocab_product_kernel(const ProductArgs g) {
-  __shared__ __attribute__((aligned(16))) T sA[kTile][kStep + kPad];
-  __shared__ __attribute__((aligned(16))) T sB[kTile][kStep + kPad];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64, lr = lane & 15, lk = lane >> 4;
-  const int m0 = blockIdx.x * kTile, n0 = blockIdx.y * kTile;
-  f32x4 acc[4][4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+// 64 lanes x 16 bytes from the buffer r at each lane's `off` into LDS at `lds`, `lds` + 16, ...; zeros past the buffer's end.
+// The compiler does not count these copies: the waits are explicit (copies_done).
+__device__ __forceinline__ void copy_to_lds(const u32x4 r, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(r) : "memory", "m0");
+}
+// All but the newest N of this wave's copies have landed, and its own LDS reads are done.
+template <int N>
+__device__ __forceinline__ void copies_done() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
 
-  auto fetch = [&](const Operand& o, int part, int r0, int k0, auto contiguous, T (*dst)[kStep + kPad]) {
-    const T* const p = (const T*)o.p + part * o.part;
-#pragma unroll 4
-    for (int i = 0; i < kTile * kStep / kThreads; ++i) {
-      const int e = i * kThreads + tid;
-      const int r = decltype(contiguous)::value ? e / kStep : e % kTile, k = decltype(contiguous)::value ? e % kStep : e / kTile;
-      const bool in = r0 + r < o.rows && k0 + k < o.depth;
-      const long long at = decltype(contiguous)::value ? (long long)(r0 + r) * o.stride + k0 + k : (long long)(k0 + k) * o.stride + r0 + r;
-      dst[r][k] = in ? p[at] : (T)0.f;
-    }
-  };
-  const int combos = g.parts == 1 ? 1 : 6;
-  for (int q = 0; q < combos; ++q) {
-    const int pa = g.parts == 1 ? 0 : kPartA[q], pb = g.parts == 1 ? 0 : kPartB[q];
-    for (int k0 = 0; k0 < g.k; k0 += kStep) {
-      __syncthreads();
-      fetch(g.a, pa, m0, k0, std::integral_constant<bool, AK>{}, sA);
-      fetch(g.b, pb, n0, k0, std::integral_constant<bool, BK>{}, sB);
-      __syncthreads();
-      uint4 fa[4], fb[4];
+// Which parts of A and B the six products of three parts each take, the smallest first: two bits a product.
+constexpr uint32_t kPartA = 2u | 1u << 2 | 0u << 4 | 1u << 6 | 0u << 8 | 0u << 10;
+constexpr uint32_t kPartB = 0u | 1u << 2 | 2u << 4 | 0u << 6 | 1u << 8 | 0u << 10;
+
+// One operand's tile of R rows: a step of it is R x 32 numbers, 64 R bytes of LDS.
+//   k contiguous: [row][4 pieces of 8 k], piece c of row r at place c ^ (r >> 1 & 3), so that eight lanes side by side, which
+//   read one piece of eight rows, meet eight different groups of four banks;
+//   k strided: [k][R / 16 pieces of 16 rows], piece u of row k at place u ^ {0, 2, 5, 7}[k & 3] (R = 64: u ^ (k & 3)): a
+//   transposing read takes one piece of four k in 16 lanes, and two neighbouring ones in 32.
+// The memory pipeline writes LDS in the order of the lanes, so the places are chosen by what each lane asks for.
+template <class T, bool K, int R>
+struct Tile {
+  static constexpr int kBytes = R * kStep * 2;
+  static constexpr int kCopies = kBytes / 4096;        // per wave of four
+  static_assert(kBytes % 4096 == 0, "whole copies for each of four waves");
+  uint32_t off[kCopies];
+  uint32_t chunk;                  // k contiguous: first k of the lane's piece
+  const char* base;                // of the tile at k = 0, part 0
+  long long step, part;            // bytes
+  long long limit;                 // k contiguous: bytes from base to the end of the last row
+  uint32_t read;                   // byte of the lane's first fragment read
+
+  __device__ __forceinline__ static uint32_t mix(uint32_t k) { return R == 64 ? k & 3u : (0x7520u >> (4 * (k & 3u))) & 7u; }
+
+  // wave and lane as the copies are dealt, first: this wave's first row within the tile
+  __device__ __forceinline__ void init(const Operand& o, int r0, int wave, int lane, int first) {
+    const long long row = o.stride * 2;
+    part = o.part * 2;
+    if constexpr (K) {
+      base = (const char*)o.p + (long long)r0 * row;
+      step = kStep * 2;
+      limit = (long long)(min(o.rows - r0, R) - 1) * row + (long long)o.depth * 2;
+      const uint32_t l = lane;
+      chunk = (l & 3u) ^ (l >> 3 & 3u);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        fa[i] = *(const uint4*)&sA[wm + i * 16 + lr][lk * 8];
-        fb[i] = *(const uint4*)&sB[wn + i * 16 + lr][lk * 8];
+      for (int j = 0; j < kCopies; ++j) off[j] = (uint32_t)((wave * kCopies + j) * 16 + (lane >> 2)) * (uint32_t)row + chunk * 16u;
+      chunk *= 8u;
+      const uint32_t r = first + (lane & 31);
+      read = r * 64u + ((uint32_t)(lane >> 5) ^ (r >> 1 & 3u)) * 16u;
+    } else {
+      base = (const char*)o.p + (long long)r0 * 2;
+      step = kStep * row;
+      limit = row;
+      chunk = (uint32_t)r0 * 2u;
+#pragma unroll
+      for (int j = 0; j < kCopies; ++j) {
+        const uint32_t u = (uint32_t)(wave * kCopies + j) * 64u + lane, k = u / (R / 8), c = u % (R / 8);
+        off[j] = k * (uint32_t)row + (((c >> 1) ^ mix(k)) * 2u + (c & 1u)) * 16u;
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = mfma<T>(fa[i], fb[j], acc[i][j]);
+      // lane 16 g + i reads four rows at k = 8 (g >> 1) + i / 4, piece first / 16 + (g & 1)
+      const uint32_t k = (uint32_t)(lane >> 5) * 8u + (lane >> 2 & 3u);
+      read = k * (R * 2u) + ((((uint32_t)first >> 4) + (lane >> 4 & 1u)) ^ mix(k)) * 32u + (lane & 3u) * 8u;
     }
   }
+  // The buffer of the next copies: aimed at k = 0 of a part, then moved on a step at a time.
+  uint64_t at;
+  long long left;                  // bytes from there to the end of the operand
+  __device__ __forceinline__ void aim(uint32_t p, int depth) {
+    at = (uint64_t)(uintptr_t)base + (uint64_t)p * (uint64_t)part;
+    left = K ? limit : (long long)depth * limit - (long long)chunk;
+  }
+  __device__ __forceinline__ void move() {
+    at += (uint64_t)step;
+    left -= step;
+  }
+  __device__ __forceinline__ u32x4 buffer() const {
+    u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32), (uint32_t)max(min(left, 0x7fffff00ll), 0ll), 0x00020000u};
+    return r;
+  }
+  __device__ __forceinline__ void copy(const u32x4& r, int j, int wave, uint32_t lds, int k0, int depth) const {
+    uint32_t o = off[j];
+    if constexpr (K) o = k0 + (int)chunk < depth ? o : 0xfffffff0u;      // (the row behind it is somebody else's)
+    copy_to_lds(r, o, lds + (uint32_t)(wave * kCopies + j) * 1024u);
+  }
+  // Fragment of rows first + 32 b .. + 31, k = 16 h .. 16 h + 15: one read, or its half j of two.
+  static constexpr int kReads = K ? 1 : 2;
+  __device__ __forceinline__ void fragment(const unsigned char* slot, int b, int h, int j, uint4& f) const {
+    if constexpr (K) {
+      f = *(const uint4*)(slot + ((read + b * 2048) ^ (h * 32)));
+    } else {
+      // rows 32 b further: pieces 2 b further, under the same exclusive or (first is a multiple of 32 b's range)
+      const uint32_t at = ((read ^ (uint32_t)(b * 64)) + h * (16 * R * 2) + j * (4 * R * 2));
+      const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(slot + at));
+      const uint2 w = __builtin_bit_cast(uint2, v);
+      if (j == 0) f.x = w.x, f.y = w.y;
+      else f.z = w.x, f.w = w.y;
+    }
+  }
+};
 
-  // acc[i][j][r]: m = wm + 16 i + 4 lk + r, n = wn + 16 j + lr
+// Workgroup of four waves: WM x WN of them, each RB x CB blocks of 32 x 32 results.
+//
+// A step is 32 of the contraction.  LDS holds four of them; the fragments of a step are read into registers while the step
+// before is multiplied, and the copies of the fourth next one are sent out, one or two between each two MFMAs.  One barrier
+// a step: behind it every wave's copies of step s + 1 have landed and nobody reads slot s % 4 any more.
+template <class T, bool AK, bool BK, int EPI, int RB, int CB, int WM, int WN>
+__global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const ProductArgs g) {
+  constexpr int BM = 32 * RB * WM, BN = 32 * CB * WN;
+  typedef Tile<T, AK, BM> TA;
+  typedef Tile<T, BK, BN> TB;
+  constexpr int kSlot = TA::kBytes + TB::kBytes, kCopies = TA::kCopies + TB::kCopies;
+  __shared__ __attribute__((aligned(1024))) unsigned char sRing[kSlots * kSlot];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ln = lane & 31, lh = lane >> 5;
+  const int wm = (wave % WM) * 32 * RB, wn = (wave / WM) * 32 * CB;
+  // Runs of consecutive work items per XCD; eight tiles of n by as many of m as it has workgroups.
+  int mt, nt;
+  {
+    const unsigned W = gridDim.x, L = blockIdx.x, xcd = L & 7u, q = W >> 3, r = W & 7u;
+    const unsigned item = xcd * q + min(xcd, r) + (L >> 3);
+    const unsigned nmt = (unsigned)(g.m + BM - 1) / BM, nnt = (unsigned)(g.n + BN - 1) / BN;
+    const unsigned group = item / (8 * nmt), first = group * 8, width = min(8u, nnt - first), in = item - first * nmt;
+    mt = (int)(in / width);
+    nt = (int)(first + in % width);
+  }
+  const int m0 = mt * BM, n0 = nt * BN;
+  TA A;
+  TB B;
+  A.init(g.a, m0, wave, lane, wm);
+  B.init(g.b, n0, wave, lane, wn);
+  const int depth_a = g.a.depth, depth_b = g.b.depth;
+  const int ksteps = (g.k + kStep - 1) / kStep, total = g.parts == 1 ? ksteps : 6 * ksteps;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sRing;
+
+  // The next copies: product of parts, k, slot.  Past the last one everything is behind the buffers' ends.
+  int cq = 0, ck = 0, cs = 0;
+  u32x4 ra, rb;
+  A.aim(g.parts == 1 ? 0u : kPartA & 3u, depth_a);
+  B.aim(g.parts == 1 ? 0u : kPartB & 3u, depth_b);
+  ra = A.buffer();
+  rb = B.buffer();
+  auto copy = [&](int j) {
+    if (j < TA::kCopies) A.copy(ra, j, wave, lds0 + (uint32_t)(cs * kSlot), ck, depth_a);
+    else B.copy(rb, j - TA::kCopies, wave, lds0 + (uint32_t)(cs * kSlot + TA::kBytes), ck, depth_b);
+  };
+  auto next = [&] {
+    cs = (cs + 1) & (kSlots - 1);
+    ck += kStep;
+    A.move();
+    B.move();
+    if (ck >= g.k) {
+      ck = 0;
+      ++cq;
+      if (g.parts > 1 && cq < 6) {
+        A.aim(kPartA >> (2 * cq) & 3u, depth_a);
+        B.aim(kPartB >> (2 * cq) & 3u, depth_b);
+      } else {
+        A.left = B.left = 0;
+      }
+    }
+    ra = A.buffer();
+    rb = B.buffer();
+  };
+  f32x16 acc[RB][CB];
+#pragma unroll
+  for (int i = 0; i < RB; ++i)
+#pragma unroll
+    for (int j = 0; j < CB; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+#pragma unroll
+  for (int s = 0; s < kSlots; ++s) {
+#pragma unroll
+    for (int j = 0; j < kCopies; ++j) copy(j);
+    next();
+  }
+  struct Frags {
+    uint4 a[2][RB], b[2][CB];
+  };
+  Frags f[2];
+  constexpr int kReadsA = 2 * RB * TA::kReads, kReadsAll = kReadsA + 2 * CB * TB::kReads;
+  auto read = [&](const unsigned char* slot, int i, Frags& to) {
+    if (i < kReadsA) {
+      const int j = i % TA::kReads, b = i / TA::kReads % RB, h = i / TA::kReads / RB;
+      A.fragment(slot, b, h, j, to.a[h][b]);
+    } else {
+      i -= kReadsA;
+      const int j = i % TB::kReads, b = i / TB::kReads % CB, h = i / TB::kReads / CB;
+      B.fragment(slot + TA::kBytes, b, h, j, to.b[h][b]);
+    }
+  };
+  copies_done<(kSlots - 1) * kCopies>();
+  __builtin_amdgcn_s_barrier();
+#pragma unroll
+  for (int i = 0; i < kReadsAll; ++i) read(sRing, i, f[0]);
+
+  auto step = [&](auto P, int s) {
+    constexpr int p = decltype(P)::value, kMfmas = 2 * RB * CB, kSpread = kMfmas > 4 ? kMfmas - 2 : kMfmas;
+    copies_done<(kSlots - 2) * kCopies>();
+    __builtin_amdgcn_s_barrier();
+    const unsigned char* const slot = sRing + ((s + 1) & (kSlots - 1)) * kSlot;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < kMfmas; ++i) {
+      const int h = i / (RB * CB), a = i / CB % RB, b = i % CB;
+      acc[a][b] = mfma<T>(f[p].a[h][a], f[p].b[h][b], acc[a][b]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = i * kReadsAll / kSpread; u < (i + 1) * kReadsAll / kSpread && u < kReadsAll; ++u) read(slot, u, f[p ^ 1]);
+#pragma unroll
+      for (int u = i * kCopies / kMfmas; u < (i + 1) * kCopies / kMfmas; ++u) copy(u);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    next();
+  };
+  int s = 0;
+  for (; s + 2 <= total; s += 2) {
+    step(std::integral_constant<int, 0>{}, s);
+    step(std::integral_constant<int, 1>{}, s + 1);
+  }
+  if (s < total) step(std::integral_constant<int, 0>{}, s);
+  copies_done<0>();
+  __syncthreads();
+
+  // acc[i][j][r]: m = wm + 32 i + 8 (r / 4) + 4 lh + r % 4, n = wn + 32 j + ln
   if constexpr (EPI == kStats) {
-    __shared__ float2 sStat[2][kTile];
+    float2* const sStat = (float2*)sRing;         // [WM][BN]
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int n = n0 + wn + 16 * j + lr;
+    for (int j = 0; j < CB; ++j) {
+      const int n = n0 + wn + 32 * j + ln;
       const uint32_t target = n < g.n ? row_of(g.targets, g.id_dtype, n, (uint32_t)g.V) : (uint32_t)g.V;
-      float top = -INFINITY;
+      // The lane's place of the target's row: 16 i + r of those above, or none.
+      const uint32_t at_row = target - (uint32_t)(g.v0 + m0 + wm);
+      const uint32_t mine = target < (uint32_t)g.V && at_row < 32u * RB && (at_row >> 2 & 1u) == (uint32_t)lh
+                                ? (at_row >> 5) * 16u + (at_row >> 3 & 3u) * 4u + (at_row & 3u) : 0xffffu;
+      int rows = g.V - (g.v0 + m0 + wm + 4 * lh);
+      asm volatile("" : "+v"(rows));       // (compared anew: 64 masks kept for all j would not fit the scalar registers)
+      float top = -INFINITY, target_z = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < RB; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int v = g.v0 + m0 + wm + 16 * i + 4 * lk + r;
-          acc[i][j][r] *= g.scale;
-          if (v < g.V) top = fmaxf(top, acc[i][j][r]);
-          if ((uint32_t)v == target && v < g.V) g.target_z[n] = acc[i][j][r];
+        for (int r = 0; r < 16; ++r) {
+          float z = acc[i][j][r] * g.scale;
+          target_z = mine == (uint32_t)(16 * i + r) ? z : target_z;
+          z = 32 * i + 8 * (r >> 2) + (r & 3) < rows ? z : -INFINITY;
+          top = fmaxf(top, z);
+          acc[i][j][r] = z;
         }
-      top = fmaxf(top, __shfl_xor(top, 16));
+      if (mine != 0xffffu) g.target_z[n] = target_z;
       top = fmaxf(top, __shfl_xor(top, 32));
       const float at = fminf(fmaxf(top, -FLT_MAX), FLT_MAX);      // (finite, so that nothing below subtracts infinities)
       float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < RB; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (g.v0 + m0 + wm + 16 * i + 4 * lk + r < g.V) sum += __expf(acc[i][j][r] - at);
-      sum += __shfl_xor(sum, 16);
+        for (int r = 0; r < 16; ++r) sum += __expf(acc[i][j][r] - at);
       sum += __shfl_xor(sum, 32);
-      if (lk == 0) sStat[wave & 1][wn + 16 * j + lr] = make_float2(at, sum);
+      if (lh == 0) sStat[(wave % WM) * BN + wn + 32 * j + ln] = make_float2(at, sum);
     }
     __syncthreads();
-    if (tid < kTile && n0 + tid < g.n) {
-      const float2 x = sStat[0][tid], y = sStat[1][tid];
-      const float at = fmaxf(x.x, y.x);
-      g.stats[(long long)((g.v0 + m0) / kTile) * g.n + n0 + tid] = make_float2(at, x.y * __expf(x.x - at) + y.y * __expf(y.x - at));
-    }
+    for (int c = tid; c < BN; c += kThreads)
+      if (n0 + c < g.n) {
+        float at = sStat[c].x, sum = 0.f;
+#pragma unroll
+        for (int w = 1; w < WM; ++w) at = fmaxf(at, sStat[w * BN + c].x);
+#pragma unroll
+        for (int w = 0; w < WM; ++w) sum += sStat[w * BN + c].y * __expf(sStat[w * BN + c].x - at);
+        g.stats[(long long)((g.v0 + m0) / BM) * g.n + n0 + c] = make_float2(at, sum);
+      }
   } else if constexpr (EPI == kGradS) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int n = n0 + wn + 16 * j + lr;
+    for (int j = 0; j < CB; ++j) {
+      const int n = n0 + wn + 32 * j + ln;
       if (n >= g.n) continue;
       const uint32_t target = row_of(g.targets, g.id_dtype, n, (uint32_t)g.V);
       const float lse = g.lse[n], weight = g.weight[n];
+      const bool named = target < (uint32_t)g.V;
+      const int m_first = m0 + wm + 4 * lh;
+      int rows = named ? g.V - (g.v0 + m_first) : 0, hit = named ? (int)(target - (uint32_t)(g.v0 + m_first)) : -1;
+      asm volatile("" : "+v"(rows), "+v"(hit));
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < RB; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int m = m0 + wm + 16 * i + 4 * lk + r, v = g.v0 + m;
+        for (int q = 0; q < 4; ++q) {
+          const int m = m_first + 32 * i + 8 * q;
           if (m >= g.ds_stride) continue;
-          float d = 0.f;
-          if (v < g.V && target < (uint32_t)g.V) d = (__expf(acc[i][j][r] * g.scale - lse) - ((uint32_t)v == target ? 1.f : 0.f)) * weight;
+          float d[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int at = 32 * i + 8 * q + r;
+            const float p = __expf(acc[i][j][4 * q + r] * g.scale - lse);
+            d[r] = at < rows ? (at == hit ? p - 1.f : p) * weight : 0.f;
+          }
           T* dst = (T*)g.ds + (long long)n * g.ds_stride + m;
           for (int p = 0; p < g.parts; ++p) {
-            const T hi = (T)d;
-            dst[p * g.ds_part] = hi;
-            d -= (float)hi;
+            typedef T T4 __attribute__((ext_vector_type(4)));
+            T4 t;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              t[r] = (T)d[r];
+              d[r] -= (float)t[r];
+            }
+            *(T4*)(dst + p * g.ds_part) = t;
           }
         }
     }
   } else {
     const float factor = g.factor ? *g.factor : 1.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int n = n0 + wn + 16 * j + lr;
+    for (int j = 0; j < CB; ++j) {
+      const int n = n0 + wn + 32 * j + ln;
       if (n >= g.n) continue;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < RB; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int m = m0 + wm + 16 * i + 4 * lk + r;
+        for (int r = 0; r < 16; ++r) {
+          const int m = m0 + wm + 32 * i + 8 * (r >> 2) + 4 * lh + (r & 3);
           if (m < g.m) store_any(g.out, g.out_dtype, (long long)n * g.out_stride + m, acc[i][j][r] * factor, g.add);
         }
     }
@@ -320,8 +520,8 @@ Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
 
 template <class T, bool AK, bool BK, int EPI>
 hipError_t launch_product(const ProductArgs& g, hipStream_t s) {
-  const dim3 grid((unsigned)((g.m + kTile - 1) / kTile), (unsigned)((g.n + kTile - 1) / kTile));
-  hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI>), grid, dim3(kThreads), 0, s, g);
+  const long long tiles = (long long)((g.m + kTile - 1) / kTile) * ((g.n + kTile - 1) / kTile);
+  hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 4, 4, 2, 2>), dim3((unsigned)tiles), dim3(kThreads), 0, s, g);
   return hipGetLastError();
 }
 
@@ -355,7 +555,7 @@ kan_status table_rows(const VocabArgs& a, const Plan& p, unsigned char* ws, int 
     *out = {src, a.D, 0, rows, a.D};
     return KAN_OK;
   }
-  *out = {ws + p.table, p.width, rows * p.width, rows, a.D};
+  *out = {ws + p.table, p.width, rows * p.width, rows, (int)p.width};
   return run_named("kan_vocab_pack", s, [&] { return pack(src, rows, a.D, p.width, a.dtype, nullptr, 0, 0, ws + p.table, s); });
 }
 
@@ -379,11 +579,11 @@ kan_status run_vocab_loss(const VocabArgs& a, hipStream_t s) {
     g.stats = (float2*)(ws + p.stats);
     g.target_z = (float*)(ws + p.target_z);
     kan_status st;
-    g.b = {a.h, a.D, 0, (int)a.N, a.D};
+    g.b = {a.h, a.D, 0, (int)a.N, a.D};      // (packed rows: zeros up to the next multiple of 64)
     if (p.pack_table) {
       st = run_named("kan_vocab_pack", s, [&] { return pack(a.h, a.N, a.D, p.width, a.dtype, nullptr, 0, 0, ws + p.h, s); });
       if (st != KAN_OK) return st;
-      g.b = {ws + p.h, p.width, a.N * p.width, (int)a.N, a.D};
+      g.b = {ws + p.h, p.width, a.N * p.width, (int)a.N, (int)p.width};
     }
     for (int v0 = 0, i = 0; i < p.pieces; ++i, v0 += p.piece) {
       g.v0 = v0;
@@ -415,7 +615,7 @@ kan_status run_vocab_grad(const VocabArgs& a, hipStream_t s) {
     if (st != KAN_OK) return st;
     st = run_named("kan_vocab_pack", s, [&] { return pack(a.h, a.N, a.D, p.width, a.dtype, a.targets, a.id_dtype, a.V, ws + p.h, s); });
     if (st != KAN_OK) return st;
-    const Operand h = {ws + p.h, p.width, a.N * p.width, (int)a.N, a.D};
+    const Operand h = {ws + p.h, p.width, a.N * p.width, (int)a.N, (int)p.width};
     for (int v0 = 0, i = 0; i < p.pieces; ++i, v0 += p.piece) {
       const int rows = std::min(p.piece, a.V - v0);
       ProductArgs g = {};
@@ -444,7 +644,7 @@ kan_status run_vocab_grad(const VocabArgs& a, hipStream_t s) {
       g.m = a.D;
       g.k = rows;
       g.a = {table.p, table.stride, table.part, a.D, rows};
-      g.b = {ws + p.ds, p.piece, g.ds_part, (int)a.N, rows};
+      g.b = {ws + p.ds, p.piece, g.ds_part, (int)a.N, (rows + 7) / 8 * 8};      // (zeros behind the last row)
       g.out = direct ? a.dh : (void*)(ws + p.dh);
       g.out_stride = a.D;
       g.out_dtype = direct ? a.dtype : KAN_F32;
