@@ -53,34 +53,49 @@ struct Operand {
   int rows, depth;
 };
 
-enum Epilogue : int { kStats, kGradS, kGradRows };
+enum Epilogue : int { kStats, kGradS, kGradRows, kGradTable };
 
 struct ProductArgs {
   Operand a, b;
   int m, n, k;               // sizes of the product
+  const int* count;          // null, or how many of n (kGradTable: of k) there are
   int parts;                 // 1, or 3: the operands' parts
+  int splits;                // shares of the contraction, each with a slice of its own in out
   // kStats, kGradS: m = rows of the table from `v0` on, n = tokens
   int v0, V;
   float scale;
-  const void* targets;
+  const void* targets;       // kGradS: 32-bit rows of the table
   int id_dtype;
   float2* stats;             // [tile of the table][tokens]
   float* target_z;
   const float *lse, *weight;
   void* ds;                  // [part][n][ds_stride]
   long long ds_stride, ds_part;
-  // kGradRows: out[n][m], in the type of the rows or added to fp32 sums
+  // kGradRows, kGradTable: out[n][m]; kGradRows: row n at place rows[n] of it
   void* out;
-  long long out_stride;
-  int out_dtype;             // type of out
+  long long out_stride, out_slice;
+  const int* rows;
+  int out_dtype;
   int add;                   // add onto it
   const float* factor;       // null, or what the sums are multiplied with
 };
 
-__device__ __forceinline__ void store_any(void* p, int dtype, long long at, float v, bool add) {
-  if (dtype == KAN_F32) ((float*)p)[at] = add ? ((float*)p)[at] + v : v;
-  else if (dtype == KAN_F16) ((f16*)p)[at] = (f16)(add ? (float)((f16*)p)[at] + v : v);
-  else ((bf16*)p)[at] = (bf16)(add ? (float)((bf16*)p)[at] + v : v);
+// Columns c .. c + 7 of a row of D, added onto what is there or not.
+__device__ __forceinline__ void store_any(void* p, int dtype, long long row, int c, int D, float (&v)[8], bool add) {
+  auto put = [&](auto t) {
+    typedef decltype(t) T;
+    T* const at = (T*)p + row;
+    if (add) {
+      float old[8];
+      load_cols(at, c, D, old);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += old[i];
+    }
+    store_cols(at, c, D, v);
+  };
+  if (dtype == KAN_F32) put(float{});
+  else if (dtype == KAN_F16) put(f16{});
+  else put(bf16{});
 }
 
 // 64 lanes x 16 bytes from the buffer r at each lane's `off` into LDS at `lds`, `lds` + 16, ...; zeros past the buffer's end.
@@ -148,12 +163,13 @@ struct Tile {
       read = k * (R * 2u) + ((((uint32_t)first >> 4) + (lane >> 4 & 1u)) ^ mix(k)) * 32u + (lane & 3u) * 8u;
     }
   }
-  // The buffer of the next copies: aimed at k = 0 of a part, then moved on a step at a time.
+  // The buffer of the next copies: aimed at some k of a part, then moved on a step at a time.
   uint64_t at;
   long long left;                  // bytes from there to the end of the operand
-  __device__ __forceinline__ void aim(uint32_t p, int depth) {
-    at = (uint64_t)(uintptr_t)base + (uint64_t)p * (uint64_t)part;
-    left = K ? limit : (long long)depth * limit - (long long)chunk;
+  __device__ __forceinline__ void aim(uint32_t p, int depth, int k0) {
+    const long long from = (long long)(k0 / kStep) * step;
+    at = (uint64_t)(uintptr_t)base + (uint64_t)((long long)p * part + from);
+    left = (K ? limit : (long long)depth * limit - (long long)chunk) - from;
   }
   __device__ __forceinline__ void move() {
     at += (uint64_t)step;
@@ -199,12 +215,15 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ln = lane & 31, lh = lane >> 5;
   const int wm = (wave % WM) * 32 * RB, wn = (wave / WM) * 32 * CB;
+  const int n_here = EPI != kGradTable && g.count ? min(g.n, *g.count) : g.n, k_here = EPI == kGradTable && g.count ? min(g.k, *g.count) : g.k;
   // Runs of consecutive work items per XCD; eight tiles of n by as many of m as it has workgroups.
-  int mt, nt;
+  int mt, nt, split;
   {
-    const unsigned W = gridDim.x, L = blockIdx.x, xcd = L & 7u, q = W >> 3, r = W & 7u;
-    const unsigned item = xcd * q + min(xcd, r) + (L >> 3);
-    const unsigned nmt = (unsigned)(g.m + BM - 1) / BM, nnt = (unsigned)(g.n + BN - 1) / BN;
+    const unsigned nmt = (unsigned)(g.m + BM - 1) / BM, nnt = (unsigned)(n_here + BN - 1) / BN, tiles = nmt * nnt, W = tiles * (unsigned)g.splits;
+    const unsigned L = blockIdx.x, xcd = L & 7u, q = W >> 3, r = W & 7u;
+    if (L >= W) return;
+    const unsigned work = xcd * q + min(xcd, r) + (L >> 3), item = work % tiles;
+    split = (int)(work / tiles);
     const unsigned group = item / (8 * nmt), first = group * 8, width = min(8u, nnt - first), in = item - first * nmt;
     mt = (int)(in / width);
     nt = (int)(first + in % width);
@@ -214,15 +233,16 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
   TB B;
   A.init(g.a, m0, wave, lane, wm);
   B.init(g.b, n0, wave, lane, wn);
-  const int depth_a = g.a.depth, depth_b = g.b.depth;
-  const int ksteps = (g.k + kStep - 1) / kStep, total = g.parts == 1 ? ksteps : 6 * ksteps;
+  const int depth_a = min(g.a.depth, AK ? g.a.depth : k_here), depth_b = min(g.b.depth, BK ? g.b.depth : k_here);
+  const int ksteps = (k_here + kStep - 1) / kStep, all = g.parts == 1 ? ksteps : 6 * ksteps;
+  const int s0 = (int)((long long)all * split / g.splits), total = (int)((long long)all * (split + 1) / g.splits) - s0;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sRing;
 
   // The next copies: product of parts, k, slot.  Past the last one everything is behind the buffers' ends.
-  int cq = 0, ck = 0, cs = 0;
+  int cq = g.parts == 1 ? 0 : s0 / max(ksteps, 1), ck = (s0 - cq * ksteps) * kStep, cs = 0;
   u32x4 ra, rb;
-  A.aim(g.parts == 1 ? 0u : kPartA & 3u, depth_a);
-  B.aim(g.parts == 1 ? 0u : kPartB & 3u, depth_b);
+  A.aim(g.parts == 1 ? 0u : kPartA >> (2 * cq) & 3u, depth_a, ck);
+  B.aim(g.parts == 1 ? 0u : kPartB >> (2 * cq) & 3u, depth_b, ck);
   ra = A.buffer();
   rb = B.buffer();
   auto copy = [&](int j) {
@@ -234,12 +254,12 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
     ck += kStep;
     A.move();
     B.move();
-    if (ck >= g.k) {
+    if (ck >= k_here) {
       ck = 0;
       ++cq;
       if (g.parts > 1 && cq < 6) {
-        A.aim(kPartA >> (2 * cq) & 3u, depth_a);
-        B.aim(kPartB >> (2 * cq) & 3u, depth_b);
+        A.aim(kPartA >> (2 * cq) & 3u, depth_a, 0);
+        B.aim(kPartB >> (2 * cq) & 3u, depth_b, 0);
       } else {
         A.left = B.left = 0;
       }
@@ -310,38 +330,53 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
 
   // acc[i][j][r]: m = wm + 32 i + 8 (r / 4) + 4 lh + r % 4, n = wn + 32 j + ln
   if constexpr (EPI == kStats) {
+    // In units of log 2: the exponentials are the hardware's, of base 2.
     float2* const sStat = (float2*)sRing;         // [WM][BN]
+    const float scale = g.scale * 1.44269504088896f;
+    const int first_row = g.v0 + m0 + wm;
 #pragma unroll
     for (int j = 0; j < CB; ++j) {
       const int n = n0 + wn + 32 * j + ln;
       const uint32_t target = n < g.n ? row_of(g.targets, g.id_dtype, n, (uint32_t)g.V) : (uint32_t)g.V;
       // The lane's place of the target's row: 16 i + r of those above, or none.
-      const uint32_t at_row = target - (uint32_t)(g.v0 + m0 + wm);
+      const uint32_t at_row = target - (uint32_t)first_row;
       const uint32_t mine = target < (uint32_t)g.V && at_row < 32u * RB && (at_row >> 2 & 1u) == (uint32_t)lh
                                 ? (at_row >> 5) * 16u + (at_row >> 3 & 3u) * 4u + (at_row & 3u) : 0xffffu;
-      int rows = g.V - (g.v0 + m0 + wm + 4 * lh);
+      if (__any(mine != 0xffffu)) {
+        float z = 0.f;
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) z = mine == (uint32_t)(16 * i + r) ? acc[i][j][r] : z;
+        if (mine != 0xffffu) g.target_z[n] = z * g.scale;
+      }
+      int rows = g.V - (first_row + 4 * lh);
       asm volatile("" : "+v"(rows));       // (compared anew: 64 masks kept for all j would not fit the scalar registers)
-      float top = -INFINITY, target_z = 0.f;
+      const bool whole = first_row + 32 * RB <= g.V;
+      float z[RB][16], top = -INFINITY, sum = 0.f;
 #pragma unroll
       for (int i = 0; i < RB; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float z = acc[i][j][r] * g.scale;
-          target_z = mine == (uint32_t)(16 * i + r) ? z : target_z;
-          z = 32 * i + 8 * (r >> 2) + (r & 3) < rows ? z : -INFINITY;
-          top = fmaxf(top, z);
-          acc[i][j][r] = z;
-        }
-      if (mine != 0xffffu) g.target_z[n] = target_z;
+        for (int r = 0; r < 16; ++r) z[i][r] = acc[i][j][r] * scale;
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) z[i][r] = 32 * i + 8 * (r >> 2) + (r & 3) < rows ? z[i][r] : -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, z[i][r]);
       top = fmaxf(top, __shfl_xor(top, 32));
       const float at = fminf(fmaxf(top, -FLT_MAX), FLT_MAX);      // (finite, so that nothing below subtracts infinities)
-      float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < RB; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum += __expf(acc[i][j][r] - at);
+        for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(z[i][r] - at);
       sum += __shfl_xor(sum, 32);
       if (lh == 0) sStat[(wave % WM) * BN + wn + 32 * j + ln] = make_float2(at, sum);
+      __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();
     for (int c = tid; c < BN; c += kThreads)
@@ -350,80 +385,170 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
 #pragma unroll
         for (int w = 1; w < WM; ++w) at = fmaxf(at, sStat[w * BN + c].x);
 #pragma unroll
-        for (int w = 0; w < WM; ++w) sum += sStat[w * BN + c].y * __expf(sStat[w * BN + c].x - at);
+        for (int w = 0; w < WM; ++w) sum += sStat[w * BN + c].y * __builtin_amdgcn_exp2f(sStat[w * BN + c].x - at);
         g.stats[(long long)((g.v0 + m0) / BM) * g.n + n0 + c] = make_float2(at, sum);
       }
-  } else if constexpr (EPI == kGradS) {
-#pragma unroll
-    for (int j = 0; j < CB; ++j) {
-      const int n = n0 + wn + 32 * j + ln;
-      if (n >= g.n) continue;
-      const uint32_t target = row_of(g.targets, g.id_dtype, n, (uint32_t)g.V);
-      const float lse = g.lse[n], weight = g.weight[n];
-      const bool named = target < (uint32_t)g.V;
-      const int m_first = m0 + wm + 4 * lh;
-      int rows = named ? g.V - (g.v0 + m_first) : 0, hit = named ? (int)(target - (uint32_t)(g.v0 + m_first)) : -1;
-      asm volatile("" : "+v"(rows), "+v"(hit));
-#pragma unroll
-      for (int i = 0; i < RB; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int m = m_first + 32 * i + 8 * q;
-          if (m >= g.ds_stride) continue;
-          float d[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int at = 32 * i + 8 * q + r;
-            const float p = __expf(acc[i][j][4 * q + r] * g.scale - lse);
-            d[r] = at < rows ? (at == hit ? p - 1.f : p) * weight : 0.f;
-          }
-          T* dst = (T*)g.ds + (long long)n * g.ds_stride + m;
-          for (int p = 0; p < g.parts; ++p) {
-            typedef T T4 __attribute__((ext_vector_type(4)));
-            T4 t;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              t[r] = (T)d[r];
-              d[r] -= (float)t[r];
-            }
-            *(T4*)(dst + p * g.ds_part) = t;
-          }
-        }
-    }
   } else {
-    const float factor = g.factor ? *g.factor : 1.f;
+    // Blocks of 32 rows n go through LDS, each wave's through its own part, so that 4 RB lanes write the pieces of one row:
+    // row r's four columns u at place u ^ r.
+    constexpr int kUnits = 8 * RB, kGroup = 4 * RB;
+    float4* const mine = (float4*)sRing + wave * (32 * kUnits);
+    const float factor = EPI != kGradS && g.factor ? *g.factor : 1.f;
 #pragma unroll
     for (int j = 0; j < CB; ++j) {
-      const int n = n0 + wn + 32 * j + ln;
-      if (n >= g.n) continue;
+      const int nb = n0 + wn + 32 * j;
+      if (nb >= n_here) break;
+      if constexpr (EPI == kGradS) {
+        const int n = min(nb + ln, n_here - 1);
+        const float lse = g.lse[n] * 1.44269504088896f, weight = g.weight[n], scale = g.scale * 1.44269504088896f;
+        const int m_first = g.v0 + m0 + wm + 4 * lh;
+        int rows = g.V - m_first, hit = ((const int*)g.targets)[n] - m_first;
+        asm volatile("" : "+v"(rows), "+v"(hit));
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int at = 32 * i + 8 * (r >> 2) + (r & 3);
+            const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], scale, -lse));
+            acc[i][j][r] = at < rows ? (at == hit ? p - 1.f : p) * weight : 0.f;
+          }
+      }
 #pragma unroll
       for (int i = 0; i < RB; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int m = m0 + wm + 32 * i + 8 * (r >> 2) + 4 * lh + (r & 3);
-          if (m < g.m) store_any(g.out, g.out_dtype, (long long)n * g.out_stride + m, acc[i][j][r] * factor, g.add);
+        for (int q = 0; q < 4; ++q)
+          mine[ln * kUnits + ((8 * i + 2 * q + lh) ^ (ln & (kUnits - 1)))] =
+              make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll 4
+      for (int r = lane / kGroup; r < 32; r += 64 / kGroup) {
+        const int u = (lane % kGroup) * 2, n = nb + r, m = m0 + wm + u * 4;
+        const float4 x = mine[r * kUnits + (u ^ (r & (kUnits - 1)))], y = mine[r * kUnits + ((u + 1) ^ (r & (kUnits - 1)))];
+        if (n >= n_here) continue;
+        float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        if constexpr (EPI == kGradS) {
+          if (m >= g.ds_stride) continue;
+          T* const dst = (T*)g.ds + (long long)n * g.ds_stride + m;
+          for (int p = 0; p < g.parts; ++p) {
+            store8(dst + p * g.ds_part, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] -= (float)(T)v[i];
+          }
+        } else {
+          if (m >= g.m) continue;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] *= factor;
+          const long long row = EPI == kGradRows && g.rows ? g.rows[n] : n;
+          store_any(g.out, g.out_dtype, split * g.out_slice + row * g.out_stride, m, g.m, v, g.add);
         }
+      }
+      __builtin_amdgcn_wave_barrier();
     }
   }
 }
 
-// Rows in the form the products take: 16-bit parts of `width` columns (zeros behind the last).  With targets: rows whose
-// target names no row are zeros, whatever they hold.
+// Which tokens have a target that names a row: their numbers in order, from the back of the list those of the others; how
+// many; fp16: what dS is multiplied with so that the largest weight is 2^14, and the factor that takes this back.
+struct Index {
+  int* list;                 // [N]
+  int* count;
+  float *mul, *factor;
+};
+__global__ __launch_bounds__(1024) void kan_vocab_index_kernel(const float* __restrict__ dloss, const void* __restrict__ targets, int id_dtype, uint32_t V, int N,
+                                                               float scale, int half, const Index x) {
+  __shared__ int sCount[16];
+  __shared__ float sMax[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int before = 0;
+  float top = 0.f;
+  for (int n0 = 0; n0 < N; n0 += 1024) {
+    const int n = n0 + threadIdx.x;
+    const bool named = n < N && row_of(targets, id_dtype, n, V) < V;
+    const uint64_t all = __ballot(named);
+    if (lane == 0) sCount[wave] = __popcll(all);
+    __syncthreads();
+    int at = before, sum = 0;
+    for (int w = 0; w < 16; ++w) {
+      at += w < wave ? sCount[w] : 0;
+      sum += sCount[w];
+    }
+    at += __popcll(all & ((1ull << lane) - 1));
+    if (named) {
+      x.list[at] = n;
+      if (half) top = fmaxf(top, fabsf(dloss[n]));
+    } else if (n < N) {
+      x.list[N - 1 - (n - at)] = n;
+    }
+    before += sum;
+    __syncthreads();
+  }
+  for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if (lane == 0) sMax[wave] = top;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  *x.count = before;
+  for (int w = 0; w < 16; ++w) top = fmaxf(top, sMax[w]);
+  *x.mul = half ? (top > 0.f ? kHalfScale / top : 0.f) : scale;
+  *x.factor = half ? scale * (top / kHalfScale) : 1.f;
+}
+
+// Rows in the form the products take: 16-bit parts of `width` columns (zeros behind the last).
 template <class I, class T, int PARTS>
-__global__ __launch_bounds__(kThreads) void kan_vocab_pack_kernel(const I* __restrict__ src, long long rows, int D, int width, long long part,
-                                                                  const void* __restrict__ targets, int id_dtype, uint32_t V, T* __restrict__ dst) {
+__global__ __launch_bounds__(kThreads) void kan_vocab_pack_kernel(const I* __restrict__ src, long long rows, int D, int width, long long part, T* __restrict__ dst) {
   const int C = width / 8;
   const long long items = rows * C;
   for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < items; i += (long long)gridDim.x * kThreads) {
     const long long row = i / C;
     const int c = (int)(i - row * C) * 8;
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (c < D && (!targets || row_of(targets, id_dtype, row, V) < V)) load_cols(src + row * D, c, D, v);
+    if (c < D) load_cols(src + row * D, c, D, v);
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
       store8(dst + p * part + row * width + c, v);
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] -= (float)(T)v[k];
+    }
+  }
+}
+
+// The same for the tokens that count, one behind the other, with their targets, lse and weights; zeros for the gradients of
+// the others.
+struct TokenArgs {
+  const void* h;
+  const void* targets;
+  const float *lse, *dloss;
+  void *packed, *dh;
+  int* target;
+  float *lse_out, *weight;
+  Index x;
+  int N, D, width, id_dtype;
+  uint32_t V;
+};
+template <class I, class T, int PARTS>
+__global__ __launch_bounds__(kThreads) void kan_vocab_tokens_kernel(const TokenArgs a) {
+  const int C = a.width / 8, count = *a.x.count;
+  const long long items = (long long)a.N * C, part = (long long)a.N * a.width;
+  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < items; i += (long long)gridDim.x * kThreads) {
+    const long long at = i / C;
+    const int c = (int)(i - at * C) * 8;
+    const long long n = a.x.list[at];
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (at >= count) {
+      if (c < a.D) store_cols((I*)a.dh + n * a.D, c, a.D, v);
+      continue;
+    }
+    if (c < a.D) load_cols((const I*)a.h + n * a.D, c, a.D, v);
+    T* const dst = (T*)a.packed + at * a.width + c;
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+      store8(dst + p * part, v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] -= (float)(T)v[k];
+    }
+    if (c == 0) {
+      a.target[at] = (int)row_of(a.targets, a.id_dtype, n, a.V);
+      a.lse_out[at] = a.lse[n];
+      a.weight[at] = a.dloss[n] * *a.x.mul;
     }
   }
 }
@@ -435,49 +560,105 @@ __global__ __launch_bounds__(256) void kan_vocab_join_kernel(const float2* __res
   // 16 tokens a workgroup, 16 lanes share a token's tiles
   __shared__ float2 sStat[16][16];
   const int at = threadIdx.x & 15, share = threadIdx.x >> 4, n = blockIdx.x * 16 + at;
-  float top = -INFINITY, sum = 0.f;
-  if (n < N)
-    for (int t = share; t < tiles; t += 16) {
-      const float2 s = stats[(long long)t * N + n];
-      const float m = fmaxf(top, s.x);
-      sum = sum * __expf(top - m) + s.y * __expf(s.x - m);
-      top = m;
-    }
+  float top = -FLT_MAX, sum = 0.f;
+  for (int t0 = share; t0 < tiles; t0 += 16 * 16) {
+    float2 s[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s[k] = t0 + 16 * k < tiles && n < N ? stats[(long long)(t0 + 16 * k) * N + n] : make_float2(-FLT_MAX, 0.f);
+    float m = top;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) m = fmaxf(m, s[k].x);
+    sum *= __builtin_amdgcn_exp2f(top - m);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) sum += s[k].y * __builtin_amdgcn_exp2f(s[k].x - m);
+    top = m;
+  }
   sStat[share][at] = make_float2(top, sum);
   __syncthreads();
   if (share == 0 && n < N) {
     float m = top;
     for (int k = 1; k < 16; ++k) m = fmaxf(m, sStat[k][at].x);
     float s = 0.f;
-    for (int k = 0; k < 16; ++k) s += sStat[k][at].y * __expf(sStat[k][at].x - m);
-    const float l = m + __logf(s);
+    for (int k = 0; k < 16; ++k) s += sStat[k][at].y * __builtin_amdgcn_exp2f(sStat[k][at].x - m);
+    const float l = 0.693147180559945f * (m + __builtin_amdgcn_logf(s));
     lse[n] = l;
     loss[n] = row_of(targets, id_dtype, n, V) < V ? l - target_z[n] : 0.f;
   }
 }
 
-// Weights of the tokens' gradients; fp16: scaled so that the largest is 2^14, and the factor that takes this back.
-__global__ __launch_bounds__(1024) void kan_vocab_weight_kernel(const float* __restrict__ dloss, const void* __restrict__ targets, int id_dtype, uint32_t V,
-                                                                long long N, float scale, int half, float* __restrict__ weight, float* __restrict__ factor) {
-  __shared__ float sMax[16];
-  float mul = scale;
-  if (half) {
-    float top = 0.f;
-    for (long long n = threadIdx.x; n < N; n += 1024)
-      if (row_of(targets, id_dtype, n, V) < V) top = fmaxf(top, fabsf(dloss[n]));
-    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if ((threadIdx.x & 63) == 0) sMax[threadIdx.x >> 6] = top;
-    __syncthreads();
-    for (int w = 0; w < 16; ++w) top = fmaxf(top, sMax[w]);
-    mul = top > 0.f ? kHalfScale / top : 0.f;
-    if (threadIdx.x == 0) *factor = scale * top / kHalfScale;
+// dh from its slices: row i of them is token list[i]'s.
+__global__ __launch_bounds__(kThreads) void kan_vocab_round_kernel(const float* __restrict__ src, int slices, long long slice, int N, int D, const Index x, int dtype,
+                                                                   void* __restrict__ dst) {
+  const int C = (D + 7) / 8;
+  const long long items = (long long)min(*x.count, N) * C;
+  const float f = *x.factor;
+  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < items; i += (long long)gridDim.x * kThreads) {
+    const long long row = i / C;
+    const int c = (int)(i - row * C) * 8;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = 0; k < slices; ++k) {
+      float t[8];
+      load_cols(src + k * slice + row * D, c, D, t);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += t[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= f;
+    store_any(dst, dtype, (long long)x.list[row] * D, c, D, v, false);
   }
-  for (long long n = threadIdx.x; n < N; n += 1024) weight[n] = row_of(targets, id_dtype, n, V) < V ? dloss[n] * mul : 0.f;
 }
 
-__global__ __launch_bounds__(kThreads) void kan_vocab_round_kernel(const float* __restrict__ src, long long n, int dtype, const float* factor, void* __restrict__ dst) {
-  const float f = factor ? *factor : 1.f;
-  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < n; i += (long long)gridDim.x * kThreads) store_any(dst, dtype, i, src[i] * f, false);
+// ---- which tiles, and how many shares of the contraction ---------------------------------------------------------------
+constexpr int kCus = 256;
+enum TileKind : int { k256x256, k256x128, k256x64, kTileKinds };
+constexpr int kTileM[] = {256, 256, 256}, kTileN[] = {256, 128, 64};
+// Clocks of a step of 32 and of a tile's beginning and end.
+constexpr long long kStepCost[] = {1024, 600, 420}, kTileCost[] = {12000, 8000, 6000};
+
+long long tiles_of(int kind, long long m, long long n) { return ((m + kTileM[kind] - 1) / kTileM[kind]) * ((n + kTileN[kind] - 1) / kTileN[kind]); }
+
+// The tiles whose fullest CU is done first.
+int pick_tiles(long long m, long long n, long long steps, int splits, long long* cost = nullptr) {
+  int best = 0;
+  long long least = -1;
+  for (int kind = 0; kind < kTileKinds; ++kind) {
+    const long long rounds = (tiles_of(kind, m, n) * splits + kCus - 1) / kCus;
+    const long long c = rounds * (((steps + splits - 1) / splits) * kStepCost[kind] + kTileCost[kind]);
+    if (least < 0 || c < least) {
+      least = c;
+      best = kind;
+    }
+  }
+  if (cost) *cost = least;
+  return best;
+}
+
+// Shares of a long contraction that few tiles have: each adds a slice of n x m sums that is written and read once.
+int pick_splits(long long m, long long n, long long steps) {
+  int best = 1;
+  long long least = -1;
+  for (int s = 1; s <= 32 && steps / s >= 8; s *= 2) {
+    long long c;
+    pick_tiles(m, n, steps, s, &c);
+    if (s > 1) c += 4000 + m * n * 4 * s / 2000;
+    if (least < 0 || c < least) {
+      least = c;
+      best = s;
+    }
+  }
+  return best;
+}
+
+template <class T, bool AK, bool BK, int EPI>
+hipError_t launch_product(const ProductArgs& g, hipStream_t s) {
+  const long long steps = (long long)((g.k + kStep - 1) / kStep) * (g.parts == 1 ? 1 : 6);
+  const int kind = pick_tiles(g.m, g.n, steps, g.splits);
+  const dim3 grid((unsigned)(tiles_of(kind, g.m, g.n) * g.splits));
+  if (kind == k256x256) hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 4, 4, 2, 2>), grid, dim3(kThreads), 0, s, g);
+  else if (kind == k256x128) hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 4, 2, 2, 2>), grid, dim3(kThreads), 0, s, g);
+  else hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 2, 2, 4, 1>), grid, dim3(kThreads), 0, s, g);
+  return hipGetLastError();
 }
 
 struct Plan {
@@ -485,7 +666,8 @@ struct Plan {
   bool pack_table;            // the table's rows go through the workspace
   long long width;            // columns of packed rows
   int piece, pieces;          // rows of the table that are dealt with at a time
-  size_t h, table, stats, target_z, weight, factor, ds, dh, bytes;
+  int slices;                 // of dh; 0: written at once
+  size_t h, table, stats, target_z, list, target, lse, weight, scalars, ds, dh, bytes;
 };
 
 Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
@@ -500,6 +682,11 @@ Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
   if (backward) limit(kPieceBytes, p.parts * N * 2);
   p.piece = (int)std::min(piece, (long long)INT32_MAX / kVocabStep * kVocabStep);
   p.pieces = (int)((V + (long long)p.piece - 1) / p.piece);
+  if (backward) {
+    const long long steps = (std::min(p.piece, V) + kStep - 1) / kStep * (p.parts == 1 ? 1 : 6);
+    p.slices = pick_splits(D, N, steps);
+    if (p.slices == 1 && p.pieces == 1) p.slices = 0;
+  }
   size_t at = 0;
   auto take = [&](long long bytes) {
     const size_t was = at;
@@ -508,37 +695,42 @@ Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
   };
   p.h = take(backward || p.pack_table ? p.parts * N * p.width * 2 : 0);
   p.table = take(p.pack_table ? p.parts * (long long)p.piece * p.width * 2 : 0);
-  p.stats = take(backward ? 0 : (all / kTile) * N * 8);
-  p.target_z = take(backward ? 0 : N * 4);
-  p.weight = take(backward ? N * 4 : 0);
-  p.factor = take(backward ? 4 : 0);
-  p.ds = take(backward ? p.parts * N * (long long)p.piece * 2 : 0);
-  p.dh = take(backward && (p.pieces > 1) ? N * D * 4ll : 0);
+  if (!backward) {
+    p.stats = take((all / kTile) * N * 8);
+    p.target_z = take(N * 4);
+  } else {
+    p.list = take(N * 4);
+    p.target = take(N * 4);
+    p.lse = take(N * 4);
+    p.weight = take(N * 4);
+    p.scalars = take(12);
+    p.ds = take(p.parts * N * (long long)p.piece * 2);
+    p.dh = take((long long)p.slices * N * D * 4);
+  }
   p.bytes = at;
   return p;
 }
 
-template <class T, bool AK, bool BK, int EPI>
-hipError_t launch_product(const ProductArgs& g, hipStream_t s) {
-  const long long tiles = (long long)((g.m + kTile - 1) / kTile) * ((g.n + kTile - 1) / kTile);
-  hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 4, 4, 2, 2>), dim3((unsigned)tiles), dim3(kThreads), 0, s, g);
-  return hipGetLastError();
+// Launches f(I{}, T{}, parts): type of the rows, of their 16-bit parts, how many.
+template <class F>
+hipError_t with_parts(int dtype, F&& f) {
+  if (dtype == KAN_F32) return f(float{}, bf16{}, std::integral_constant<int, 3>{});
+  if (dtype == KAN_F16) return f(f16{}, f16{}, std::integral_constant<int, 1>{});
+  return f(bf16{}, bf16{}, std::integral_constant<int, 1>{});
 }
 
-hipError_t pack(const void* src, long long rows, int D, long long width, int dtype, const void* targets, int id_dtype, int V, void* dst, hipStream_t s) {
-  const long long items = rows * (width / 8);
-  const dim3 grid((unsigned)std::min((items + kThreads - 1) / kThreads, 1ll << 16));
-  const long long part = rows * width;
-  if (dtype == KAN_F32)
-    hipLaunchKernelGGL((kan_vocab_pack_kernel<float, bf16, 3>), grid, dim3(kThreads), 0, s, (const float*)src, rows, D, (int)width, part, targets, id_dtype,
-                       (uint32_t)V, (bf16*)dst);
-  else if (dtype == KAN_F16)
-    hipLaunchKernelGGL((kan_vocab_pack_kernel<f16, f16, 1>), grid, dim3(kThreads), 0, s, (const f16*)src, rows, D, (int)width, part, targets, id_dtype,
-                       (uint32_t)V, (f16*)dst);
-  else
-    hipLaunchKernelGGL((kan_vocab_pack_kernel<bf16, bf16, 1>), grid, dim3(kThreads), 0, s, (const bf16*)src, rows, D, (int)width, part, targets, id_dtype,
-                       (uint32_t)V, (bf16*)dst);
-  return hipGetLastError();
+dim3 item_grid(long long items) { return dim3((unsigned)std::min((items + kThreads - 1) / kThreads, 1ll << 15)); }
+
+kan_status pack(const void* src, long long rows, int D, long long width, int dtype, void* dst, hipStream_t s) {
+  return run_named("kan_vocab_pack", s, [&] {
+    return with_parts(dtype, [&](auto i, auto t, auto parts) {
+      typedef decltype(i) I;
+      typedef decltype(t) T;
+      hipLaunchKernelGGL((kan_vocab_pack_kernel<I, T, decltype(parts)::value>), item_grid(rows * (width / 8)), dim3(kThreads), 0, s, (const I*)src, rows, D,
+                         (int)width, rows * width, (T*)dst);
+      return hipGetLastError();
+    });
+  });
 }
 
 // f(T{}): the type of the 16-bit operands.
@@ -556,7 +748,7 @@ kan_status table_rows(const VocabArgs& a, const Plan& p, unsigned char* ws, int 
     return KAN_OK;
   }
   *out = {ws + p.table, p.width, rows * p.width, rows, (int)p.width};
-  return run_named("kan_vocab_pack", s, [&] { return pack(src, rows, a.D, p.width, a.dtype, nullptr, 0, 0, ws + p.table, s); });
+  return pack(src, rows, a.D, p.width, a.dtype, ws + p.table, s);
 }
 
 }  // namespace
@@ -572,6 +764,7 @@ kan_status run_vocab_loss(const VocabArgs& a, hipStream_t s) {
     g.n = (int)a.N;
     g.k = a.D;
     g.parts = p.parts;
+    g.splits = 1;
     g.V = a.V;
     g.scale = a.scale;
     g.targets = a.targets;
@@ -579,10 +772,9 @@ kan_status run_vocab_loss(const VocabArgs& a, hipStream_t s) {
     g.stats = (float2*)(ws + p.stats);
     g.target_z = (float*)(ws + p.target_z);
     kan_status st;
-    g.b = {a.h, a.D, 0, (int)a.N, a.D};      // (packed rows: zeros up to the next multiple of 64)
+    g.b = {a.h, a.D, 0, (int)a.N, a.D};
     if (p.pack_table) {
-      st = run_named("kan_vocab_pack", s, [&] { return pack(a.h, a.N, a.D, p.width, a.dtype, nullptr, 0, 0, ws + p.h, s); });
-      if (st != KAN_OK) return st;
+      if ((st = pack(a.h, a.N, a.D, p.width, a.dtype, ws + p.h, s)) != KAN_OK) return st;
       g.b = {ws + p.h, p.width, a.N * p.width, (int)a.N, (int)p.width};
     }
     for (int v0 = 0, i = 0; i < p.pieces; ++i, v0 += p.piece) {
@@ -603,72 +795,83 @@ kan_status run_vocab_loss(const VocabArgs& a, hipStream_t s) {
 kan_status run_vocab_grad(const VocabArgs& a, hipStream_t s) {
   const Plan p = make_plan(a.N, a.V, a.D, a.dtype, true);
   unsigned char* const ws = (unsigned char*)a.ws;
-  const int half = a.dtype == KAN_F16;
-  float* const factor = half ? (float*)(ws + p.factor) : nullptr;
-  return with_operand(a.dtype, [&](auto t) -> kan_status {
-    typedef decltype(t) T;
-    kan_status st = run_named("kan_vocab_weight", s, [&] {
-      hipLaunchKernelGGL(kan_vocab_weight_kernel, dim3(1), dim3(1024), 0, s, a.dloss, a.targets, a.id_dtype, (uint32_t)a.V, a.N, a.scale, half,
-                         (float*)(ws + p.weight), factor);
+  const int N = (int)a.N;
+  const Index x = {(int*)(ws + p.list), (int*)(ws + p.scalars), (float*)(ws + p.scalars) + 1, (float*)(ws + p.scalars) + 2};
+  kan_status st = run_named("kan_vocab_index", s, [&] {
+    hipLaunchKernelGGL(kan_vocab_index_kernel, dim3(1), dim3(1024), 0, s, a.dloss, a.targets, a.id_dtype, (uint32_t)a.V, N, a.scale, a.dtype == KAN_F16, x);
+    return hipGetLastError();
+  });
+  if (st != KAN_OK) return st;
+  const TokenArgs ta = {a.h, a.targets, a.lse, a.dloss, ws + p.h, a.dh, (int*)(ws + p.target), (float*)(ws + p.lse), (float*)(ws + p.weight), x, N, a.D,
+                        (int)p.width, a.id_dtype, (uint32_t)a.V};
+  st = run_named("kan_vocab_tokens", s, [&] {
+    return with_parts(a.dtype, [&](auto i, auto t, auto parts) {
+      hipLaunchKernelGGL((kan_vocab_tokens_kernel<decltype(i), decltype(t), decltype(parts)::value>), item_grid(N * (p.width / 8)), dim3(kThreads), 0, s, ta);
       return hipGetLastError();
     });
-    if (st != KAN_OK) return st;
-    st = run_named("kan_vocab_pack", s, [&] { return pack(a.h, a.N, a.D, p.width, a.dtype, a.targets, a.id_dtype, a.V, ws + p.h, s); });
-    if (st != KAN_OK) return st;
-    const Operand h = {ws + p.h, p.width, a.N * p.width, (int)a.N, (int)p.width};
+  });
+  if (st != KAN_OK) return st;
+  return with_operand(a.dtype, [&](auto t) -> kan_status {
+    typedef decltype(t) T;
+    const Operand h = {ws + p.h, p.width, a.N * p.width, N, (int)p.width};
     for (int v0 = 0, i = 0; i < p.pieces; ++i, v0 += p.piece) {
       const int rows = std::min(p.piece, a.V - v0);
+      const long long ds_part = a.N * (long long)p.piece;
+      Operand table;
+      if ((st = table_rows(a, p, ws, v0, rows, &table, s)) != KAN_OK) return st;
       ProductArgs g = {};
+      g.count = x.count;
       g.parts = p.parts;
+      g.splits = 1;
       g.v0 = v0;
       g.V = a.V;
       g.scale = a.scale;
-      g.targets = a.targets;
-      g.id_dtype = a.id_dtype;
-      g.lse = a.lse;
-      g.weight = (const float*)(ws + p.weight);
+      g.targets = ta.target;
+      g.lse = ta.lse_out;
+      g.weight = ta.weight;
       g.ds = ws + p.ds;
       g.ds_stride = p.piece;
-      g.ds_part = a.N * (long long)p.piece;
+      g.ds_part = ds_part;
       g.m = rows;
-      g.n = (int)a.N;
+      g.n = N;
       g.k = a.D;
-      Operand table;
-      if ((st = table_rows(a, p, ws, v0, rows, &table, s)) != KAN_OK) return st;
       g.a = table;
       g.b = h;
       st = run_named("kan_vocab_ds", s, [&] { return launch_product<T, true, true, kGradS>(g, s); });
       if (st != KAN_OK) return st;
       // dh (+)= dS T: k = rows of the piece
-      const bool direct = p.pieces == 1;
       g.m = a.D;
       g.k = rows;
+      g.splits = std::max(1, p.slices);
       g.a = {table.p, table.stride, table.part, a.D, rows};
-      g.b = {ws + p.ds, p.piece, g.ds_part, (int)a.N, (rows + 7) / 8 * 8};      // (zeros behind the last row)
-      g.out = direct ? a.dh : (void*)(ws + p.dh);
+      g.b = {ws + p.ds, p.piece, ds_part, N, (rows + 7) / 8 * 8};      // (zeros behind the last row)
+      g.out = p.slices ? (void*)(ws + p.dh) : a.dh;
       g.out_stride = a.D;
-      g.out_dtype = direct ? a.dtype : KAN_F32;
+      g.out_slice = a.N * a.D;
+      g.out_dtype = p.slices ? KAN_F32 : a.dtype;
+      g.rows = p.slices ? nullptr : x.list;
       g.add = i > 0;
-      g.factor = direct ? factor : nullptr;
+      g.factor = p.slices ? nullptr : x.factor;
       st = run_named("kan_vocab_dh", s, [&] { return launch_product<T, false, true, kGradRows>(g, s); });
       if (st != KAN_OK) return st;
       // dT (+)= dS^t h: k = tokens
       g.n = rows;
-      g.k = (int)a.N;
-      g.a = {h.p, h.stride, h.part, a.D, (int)a.N};
-      g.b = {ws + p.ds, p.piece, g.ds_part, rows, (int)a.N};
+      g.k = N;
+      g.splits = 1;
+      g.a = {h.p, h.stride, h.part, a.D, N};
+      g.b = {ws + p.ds, p.piece, ds_part, rows, N};
       g.out = (char*)a.dtable + (long long)v0 * a.D * float_bytes(a.dtype);
       g.out_dtype = a.dtype;
+      g.rows = nullptr;
       g.add = a.accumulate;
-      g.factor = factor;
-      st = run_named("kan_vocab_dtable", s, [&] { return launch_product<T, false, false, kGradRows>(g, s); });
+      g.factor = x.factor;
+      st = run_named("kan_vocab_dtable", s, [&] { return launch_product<T, false, false, kGradTable>(g, s); });
       if (st != KAN_OK) return st;
     }
-    if (p.pieces == 1) return KAN_OK;
+    if (!p.slices) return KAN_OK;
     return run_named("kan_vocab_round", s, [&] {
-      const long long n = a.N * a.D;
-      hipLaunchKernelGGL(kan_vocab_round_kernel, dim3((unsigned)std::min((n + kThreads - 1) / kThreads, 1ll << 14)), dim3(kThreads), 0, s,
-                         (const float*)(ws + p.dh), n, a.dtype, factor, a.dh);
+      hipLaunchKernelGGL(kan_vocab_round_kernel, item_grid(a.N * ((a.D + 7) / 8)), dim3(kThreads), 0, s, (const float*)(ws + p.dh), p.slices, a.N * a.D, N, a.D, x,
+                         a.dtype, a.dh);
       return hipGetLastError();
     });
   });
