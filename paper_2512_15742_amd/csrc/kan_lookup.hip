@@ -8,7 +8,7 @@
 //
 // Gradient: the sums of a row are those of a run of tokens sorted by (id, position), so the order of every sum is fixed
 // and no atomics add floats.  Up to kRankTokens tokens one launch finds each token's place by counting the tokens in
-// front of it; beyond, a radix sort with 8 bits a pass.  The sorted order is cut into chunks of equal length, whatever
+// front of it; beyond, a radix sort with 9 bits a pass.  The sorted order is cut into chunks of equal length, whatever
 // the histogram of the ids: a chunk sums its runs in fp32, writes the rows of runs that lie within it, and leaves what
 // a run has in it when the run goes on in another chunk; a last launch joins those parts in their order.  So a token
 // that is a tenth of a batch costs no more than others.
@@ -64,7 +64,8 @@ __global__ __launch_bounds__(kThreads) void kan_lookup_kernel(const T* __restric
 // ---- sorting the tokens ---------------------------------------------------------------------------------------------
 constexpr int kRankTokens = 8192;           // keys of all tokens in LDS
 constexpr int kRankThreads = 1024;          // 64 tokens, 16 waves that share the counting
-constexpr int kSortThreads = 1024, kSortPer = 16, kSortTile = kSortThreads * kSortPer;
+constexpr int kSortThreads = 1024;
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;      // a pass; two for tables of up to 2^18 rows
 constexpr int kInlineTiles = 64;            // up to here a tile adds the counts of the others itself
 
 // Zeros for every element of the gradient: blocks blockIdx.x = first .. first + blocks - 1 of a launch.
@@ -114,92 +115,103 @@ __global__ __launch_bounds__(kRankThreads) void kan_lookup_rank_kernel(const voi
   }
 }
 
-// How often each digit occurs in each tile of keys.
+// How often each digit occurs in each tile of `per` x 1024 keys.
 __global__ __launch_bounds__(kSortThreads) void kan_lookup_count_kernel(const void* __restrict__ ids, int id_dtype, const uint32_t* __restrict__ keys,
-                                                                        long long N, uint32_t V, int shift, uint32_t* __restrict__ counts,
+                                                                        long long N, uint32_t V, int shift, int per, uint32_t* __restrict__ counts,
                                                                         unsigned tiles, unsigned char* fill, long long fill_bytes) {
-  __shared__ uint32_t sHist[256];
+  __shared__ uint32_t sHist[kDigits];
   if (blockIdx.x >= tiles) {
     fill_zero(fill, fill_bytes, blockIdx.x - tiles, gridDim.x - tiles);
     return;
   }
-  if (threadIdx.x < 256) sHist[threadIdx.x] = 0;
+  if (threadIdx.x < kDigits) sHist[threadIdx.x] = 0;
   __syncthreads();
-  const long long first = (long long)blockIdx.x * kSortTile;
+  const long long first = (long long)blockIdx.x * per * kSortThreads;
 #pragma unroll 4
-  for (int r = 0; r < kSortPer; ++r) {
+  for (int r = 0; r < per; ++r) {
     const long long n = first + r * kSortThreads + threadIdx.x;
-    if (n < N) atomicAdd(&sHist[((keys ? keys[n] : row_of(ids, id_dtype, n, V)) >> shift) & 255u], 1u);
+    if (n < N) atomicAdd(&sHist[((keys ? keys[n] : row_of(ids, id_dtype, n, V)) >> shift) & (kDigits - 1)], 1u);
   }
   __syncthreads();
-  if (threadIdx.x < 256) counts[(size_t)blockIdx.x * 256 + threadIdx.x] = sHist[threadIdx.x];
+  if (threadIdx.x < kDigits) counts[(size_t)blockIdx.x * kDigits + threadIdx.x] = sHist[threadIdx.x];
 }
 
 // counts[tile][digit] -> keys of that digit in the tiles in front; their sum over all tiles behind the last tile's row.
-__global__ __launch_bounds__(256) void kan_lookup_scan_kernel(uint32_t* __restrict__ counts, unsigned tiles) {
-  __shared__ uint32_t sSum[256];
-  const unsigned digit = blockIdx.x, t = threadIdx.x, per = (tiles + 255) / 256;
+// A workgroup has 16 digits, 64 threads share the tiles of each.
+__global__ __launch_bounds__(kSortThreads) void kan_lookup_scan_kernel(uint32_t* __restrict__ counts, unsigned tiles) {
+  __shared__ uint32_t sSum[64][17];
+  const unsigned digit = blockIdx.x * 16 + (threadIdx.x & 15), t = threadIdx.x >> 4, per = (tiles + 63) / 64;
   const unsigned a = min(tiles, t * per), b = min(tiles, a + per);
   uint32_t sum = 0;
-  for (unsigned i = a; i < b; ++i) sum += counts[(size_t)i * 256 + digit];
-  sSum[t] = sum;
+#pragma unroll 8
+  for (unsigned i = a; i < b; ++i) sum += counts[(size_t)i * kDigits + digit];
+  sSum[t][threadIdx.x & 15] = sum;
   __syncthreads();
   uint32_t before = 0;
-  for (unsigned i = 0; i < t; ++i) before += sSum[i];
+  for (unsigned i = 0; i < t; ++i) before += sSum[i][threadIdx.x & 15];
   for (unsigned i = a; i < b; ++i) {
-    const uint32_t c = counts[(size_t)i * 256 + digit];
-    counts[(size_t)i * 256 + digit] = before;
+    const uint32_t c = counts[(size_t)i * kDigits + digit];
+    counts[(size_t)i * kDigits + digit] = before;
     before += c;
   }
-  if (t == 255) counts[(size_t)tiles * 256 + digit] = before;
+  if (t == 63) counts[(size_t)tiles * kDigits + digit] = before;
 }
 
-// One pass of the sort: keys that agree in the digit keep their order.  A wave takes 1024 keys in a row, 64 at a time: lanes
+// One pass of the sort: keys that agree in the digit keep their order.  A wave takes 64 PER keys in a row, 64 at a time: lanes
 // of equal digits find each other with a ballot per bit, a counter per wave and digit carries on.
+template <int PER>
 __global__ __launch_bounds__(kSortThreads) void kan_lookup_scatter_kernel(const void* __restrict__ ids, int id_dtype,
                                                                           const uint32_t* __restrict__ keys_in, const uint32_t* __restrict__ order_in,
                                                                           long long N, uint32_t V, int shift, const uint32_t* __restrict__ counts,
                                                                           unsigned tiles, int scanned, uint32_t* __restrict__ keys_out,
-                                                                          uint32_t* __restrict__ order_out) {
-  __shared__ uint32_t sOff[16][256];
-  __shared__ uint32_t sPart[2][4][256];
+                                                                          uint32_t* __restrict__ order_out, unsigned char* fill, long long fill_bytes) {
+  __shared__ uint32_t sOff[16][kDigits];
+  __shared__ uint32_t sPart[2][kDigits];
+  __shared__ uint32_t sWave[8];
+  if (blockIdx.x >= tiles) {
+    fill_zero(fill, fill_bytes, blockIdx.x - tiles, gridDim.x - tiles);
+    return;
+  }
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int i = tid; i < 16 * 256; i += kSortThreads) (&sOff[0][0])[i] = 0;
+  for (int i = tid; i < 16 * kDigits; i += kSortThreads) (&sOff[0][0])[i] = 0;
+  const long long first = (long long)blockIdx.x * PER * kSortThreads + wave * (64 * PER) + lane;
+  uint32_t key[PER], rank[PER];
+#pragma unroll
+  for (int r = 0; r < PER; ++r) {
+    const long long n = first + r * 64;
+    key[r] = n < N ? (keys_in ? keys_in[n] : row_of(ids, id_dtype, n, V)) : 0u;
+  }
   // keys of a digit in all tiles, and in those in front of this one
+  uint32_t total = 0, before = 0;
   {
-    const int digit = tid & 255, part = tid >> 8;
-    uint32_t total = 0, before = 0;
+    const int digit = tid & (kDigits - 1), part = tid >> kDigitBits;
     if (scanned) {
       if (part == 0) {
-        total = counts[(size_t)tiles * 256 + digit];
-        before = counts[(size_t)blockIdx.x * 256 + digit];
+        total = counts[(size_t)tiles * kDigits + digit];
+        before = counts[(size_t)blockIdx.x * kDigits + digit];
       }
     } else {
-      for (unsigned i = part; i < tiles; i += 4) {
-        const uint32_t c = counts[(size_t)i * 256 + digit];
+#pragma unroll 8
+      for (unsigned i = part; i < tiles; i += 2) {
+        const uint32_t c = counts[(size_t)i * kDigits + digit];
         total += c;
         before += i < blockIdx.x ? c : 0u;
       }
     }
-    sPart[0][part][digit] = total;
-    sPart[1][part][digit] = before;
+    if (part == 1) {
+      sPart[0][digit] = total;
+      sPart[1][digit] = before;
+    }
   }
   __syncthreads();
-  const long long first = (long long)blockIdx.x * kSortTile + wave * (64 * kSortPer) + lane;
-  uint32_t key[kSortPer], rank[kSortPer];
-#pragma unroll
-  for (int r = 0; r < kSortPer; ++r) {
-    const long long n = first + r * 64;
-    key[r] = n < N ? (keys_in ? keys_in[n] : row_of(ids, id_dtype, n, V)) : 0u;
-  }
   volatile uint32_t* const mine = sOff[wave];
 #pragma unroll
-  for (int r = 0; r < kSortPer; ++r) {
+  for (int r = 0; r < PER; ++r) {
     const bool live = first + r * 64 < N;
-    const uint32_t digit = (key[r] >> shift) & 255u;
+    const uint32_t digit = (key[r] >> shift) & (kDigits - 1);
     uint64_t same = __ballot(live);
 #pragma unroll
-    for (int b = 0; b < 8; ++b) {
+    for (int b = 0; b < kDigitBits; ++b) {
       const uint64_t m = __ballot((digit >> b) & 1u);
       same &= (digit >> b) & 1u ? m : ~m;
     }
@@ -209,19 +221,23 @@ __global__ __launch_bounds__(kSortThreads) void kan_lookup_scatter_kernel(const 
     if (live && (same >> lane) == 1ull) mine[digit] = rank[r] + 1;       // the last of its lanes
     __builtin_amdgcn_wave_barrier();
   }
-  __syncthreads();
-  if (tid < 256) {
-    uint32_t before = 0;
-    for (int p = 0; p < 4; ++p) before += sPart[1][p][tid];
-    // keys of smaller digits: summed in 64 lanes of four, then within the four
-    sPart[0][0][tid] += sPart[0][1][tid] + sPart[0][2][tid] + sPart[0][3][tid];
-    sPart[1][0][tid] = before;
+  uint32_t scan = 0;                  // keys of this digit and of smaller ones in its wave
+  if (tid < kDigits) {
+    total += sPart[0][tid];
+    before += sPart[1][tid];
+    scan = total;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t o = __shfl_up(scan, d);
+      if (lane >= d) scan += o;
+    }
+    if (lane == 63) sWave[wave] = scan;
   }
   __syncthreads();
-  if (tid < 256) {
-    uint32_t smaller = 0;
-    for (int d = 0; d < tid; ++d) smaller += sPart[0][0][d];
-    uint32_t at = smaller + sPart[1][0][tid];
+  if (tid < kDigits) {
+    uint32_t at = before + scan - total;
+    for (int w = 0; w < wave; ++w) at += sWave[w];
+#pragma unroll
     for (int w = 0; w < 16; ++w) {
       const uint32_t c = sOff[w][tid];
       sOff[w][tid] = at;
@@ -230,10 +246,10 @@ __global__ __launch_bounds__(kSortThreads) void kan_lookup_scatter_kernel(const 
   }
   __syncthreads();
 #pragma unroll
-  for (int r = 0; r < kSortPer; ++r) {
+  for (int r = 0; r < PER; ++r) {
     const long long n = first + r * 64;
     if (n < N) {
-      const uint32_t to = sOff[wave][(key[r] >> shift) & 255u] + rank[r];
+      const uint32_t to = sOff[wave][(key[r] >> shift) & (kDigits - 1)] + rank[r];
       keys_out[to] = key[r];
       order_out[to] = order_in ? order_in[n] : (uint32_t)n;
     }
@@ -252,18 +268,29 @@ struct SumArgs {
   float scale;
 };
 
-template <class O>
-__device__ __forceinline__ void put_row(O* dst, int c, int cols, int D, const float* sum, float scale, int accumulate) {
-  for (int i = 0; i < cols; ++i)
-    if (c + i < D) dst[c + i] = (O)(accumulate ? (float)dst[c + i] + sum[i] * scale : sum[i] * scale);
+template <int VEC, class O>
+__device__ __forceinline__ void put(O* dst, int c, int D, float (&sum)[VEC], const SumArgs& a) {
+  if constexpr (VEC == 8) {
+    float old[8];
+    if (a.accumulate) load_cols(dst, c, D, old);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = a.accumulate ? old[i] + sum[i] * a.scale : sum[i] * a.scale;
+    store_cols(dst, c, D, sum);
+  } else {
+    dst[c] = (O)(a.accumulate ? (float)dst[c] + sum[0] * a.scale : sum[0] * a.scale);
+  }
 }
 
-// Narrow rows: a lane has one column and 64 / lanes chunks share a wave; wide rows: eight columns a lane.
-template <class I, class O, int VEC>
+// Wide rows: eight columns a lane, a wave has a chunk of its own, whose keys and positions are scalars.  Narrow rows: a lane
+// has one column, and 64 / lanes chunks share a wave.  The keys of the next eight tokens are on their way while eight rows are.
+template <class I, class O, bool WIDE>
 __global__ __launch_bounds__(kThreads) void kan_lookup_sum_kernel(const I* __restrict__ dy, O* __restrict__ dtable, const SumArgs a) {
-  const int lane = threadIdx.x % a.lanes;
-  const long long chunk = (long long)blockIdx.x * (kThreads / a.lanes) + threadIdx.x / a.lanes;
-  const int c = (blockIdx.y * a.lanes + lane) * VEC;
+  constexpr int VEC = WIDE ? 8 : 1;
+  const int lanes = WIDE ? 64 : a.lanes;
+  const int lane = threadIdx.x % lanes;
+  const int group = WIDE ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : threadIdx.x / lanes;
+  const long long chunk = (long long)blockIdx.x * (kThreads / lanes) + group;
+  const int c = (blockIdx.y * lanes + lane) * VEC;
   const long long first = chunk * a.chunk, end = min(a.N, first + a.chunk);
   if (first >= a.N || c >= a.D) return;
   float sum[VEC];
@@ -276,47 +303,36 @@ __global__ __launch_bounds__(kThreads) void kan_lookup_sum_kernel(const I* __res
     if (run < a.V) {
       if (from_before || goes_on) {
         float* const p = parts + (from_before ? 0 : a.D);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i)
-          if (c + i < a.D) p[c + i] = sum[i];
+        if constexpr (WIDE) store_cols(p, c, a.D, sum);
+        else p[c] = sum[0];
       } else {
-        O* const dst = dtable + (long long)run * a.D;
-        if constexpr (VEC == 8) {
-          if (c + 8 <= a.D) {
-            float v[8], old[8];
-            if (a.accumulate) load8(dst + c, old);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = a.accumulate ? old[i] + sum[i] * a.scale : sum[i] * a.scale;
-            store8(dst + c, v);
-          } else {
-            put_row(dst, c, VEC, a.D, sum, a.scale, a.accumulate);
-          }
-        } else {
-          put_row(dst, c, VEC, a.D, sum, a.scale, a.accumulate);
-        }
+        put<VEC>(dtable + (long long)run * a.D, c, a.D, sum, a);
       }
     }
 #pragma unroll
     for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
     from_before = false;
   };
-  for (long long p = first; p < end; p += 8) {
-    uint32_t key[8], at[8];
+  uint32_t key[8], at[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {       // (the arrays are padded to a multiple of eight)
-      key[u] = a.keys[p + u];
-      at[u] = a.order[p + u];
-    }
+  for (int u = 0; u < 8; ++u) {       // (the arrays are padded: eight tokens behind the last chunk)
+    key[u] = a.keys[first + u];
+    at[u] = a.order[first + u];
+  }
+  for (long long p = first; p < end; p += 8) {
     float v[8][VEC];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const bool live = p + u < end && key[u] < a.V;
       const I* const row = dy + (long long)(live ? at[u] : 0u) * a.D;
-      if constexpr (VEC == 8) {
-        if (live) load_cols(row, c, a.D, v[u]);
-      } else {
-        if (live) v[u][0] = (float)row[c];
-      }
+      if constexpr (WIDE) load_cols(row, c, a.D, v[u]);
+      else v[u][0] = (float)row[c];
+    }
+    uint32_t key_next[8], at_next[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      key_next[u] = a.keys[p + 8 + u];
+      at_next[u] = a.order[p + 8 + u];
     }
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
@@ -325,52 +341,60 @@ __global__ __launch_bounds__(kThreads) void kan_lookup_sum_kernel(const I* __res
           flush(false);
           run = key[u];
         }
-        if (run < a.V) {
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) sum[i] += v[u][i];
-        }
+        for (int i = 0; i < VEC; ++i) sum[i] += v[u][i];
       }
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      key[u] = key_next[u];
+      at[u] = at_next[u];
     }
   }
   flush(end < a.N && a.keys[end] == run);
 }
 
-// The run that begins in a chunk and goes on behind it: its parts, in order.  16 (narrow rows) or 4 groups of lanes take a
-// share of the parts each.
-template <class O, int VEC>
-__global__ __launch_bounds__(kThreads) void kan_lookup_join_kernel(O* __restrict__ dtable, const SumArgs a, long long chunks) {
-  __shared__ float sSum[kThreads * VEC];
+// The run that begins in a chunk and goes on behind it: its parts, in order.  Groups of lanes take a share of the parts each.
+constexpr int kJoinThreads = 1024;
+template <class O, bool WIDE>
+__global__ __launch_bounds__(kJoinThreads) void kan_lookup_join_kernel(O* __restrict__ dtable, const SumArgs a, long long chunks) {
+  constexpr int VEC = WIDE ? 8 : 1;
+  __shared__ float sSum[kJoinThreads * VEC];
+  const int lanes = WIDE ? 64 : a.lanes;
   const long long chunk = blockIdx.x;
   const long long end = (chunk + 1) * a.chunk;
   if (end >= a.N) return;
-  const uint32_t run = a.keys[end];
-  if (run >= a.V || a.keys[end - 1] != run) return;
   const long long first = chunk * a.chunk;
-  if (first > 0 && a.keys[first] == run && a.keys[first - 1] == run) return;       // it began further in front
+  const uint32_t run = a.keys[end], last_in = a.keys[end - 1], first_in = a.keys[first], in_front = a.keys[max(first - 1, 0ll)];
+  if (run >= a.V || last_in != run) return;
+  if (first > 0 && first_in == run && in_front == run) return;       // it began further in front
   // chunks behind this one that the run reaches
   long long last = chunk + 1;
   for (;;) {
     const long long k = last + 1 + (threadIdx.x & 63);
-    const uint64_t on = __ballot(k < chunks && a.keys[k * a.chunk] == run);
+    const uint64_t on = __ballot(k < chunks && a.keys[min(k, chunks - 1) * a.chunk] == run);
     const int n = on == ~0ull ? 64 : __ffsll((long long)~on) - 1;
     last += n;
     if (n < 64) break;
   }
-  const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = kThreads / a.lanes;
-  const int c = (blockIdx.y * a.lanes + lane) * VEC;
+  const int lane = threadIdx.x % lanes, group = threadIdx.x / lanes, groups = kJoinThreads / lanes;
+  const int c = (blockIdx.y * lanes + lane) * VEC;
   const long long parts = last - chunk + 1, per = (parts + groups - 1) / groups;
-  const long long p0 = group * per, p1 = min(parts, p0 + per);
+  const long long p0 = group * per, p1 = c < a.D ? min(parts, p0 + per) : 0;
   float sum[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
 #pragma unroll 4
   for (long long p = p0; p < p1; ++p) {
     const float* const src = a.parts + (chunk + p) * 2 * a.D + (p == 0 ? a.D : 0);
+    float v[VEC];
+    if constexpr (WIDE) load_cols(src, c, a.D, v);
+    else v[0] = src[c];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) sum[i] += c + i < a.D ? src[c + i] : 0.f;
+    for (int i = 0; i < VEC; ++i) sum[i] += v[i];
   }
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) sSum[(group * VEC + i) * a.lanes + lane] = sum[i];
+  for (int i = 0; i < VEC; ++i) sSum[(group * VEC + i) * lanes + lane] = sum[i];
   __syncthreads();
   if (group != 0 || c >= a.D) return;
   const int busy = (int)min((long long)groups, (parts + per - 1) / per);
@@ -378,16 +402,17 @@ __global__ __launch_bounds__(kThreads) void kan_lookup_join_kernel(O* __restrict
   for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
   for (int g = 0; g < busy; ++g)
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) sum[i] += sSum[(g * VEC + i) * a.lanes + lane];
-  put_row(dtable + (long long)run * a.D, c, VEC, a.D, sum, a.scale, a.accumulate);
+    for (int i = 0; i < VEC; ++i) sum[i] += sSum[(g * VEC + i) * lanes + lane];
+  put<VEC>(dtable + (long long)run * a.D, c, a.D, sum, a);
 }
 
 // ---- plan of a gradient ----------------------------------------------------------------------------------------------
 struct GradPlan {
   bool rank;                 // one counting launch in place of the radix sort
-  unsigned tiles;            // radix sort
-  int passes;
-  int chunk, lanes, vec;
+  unsigned tiles;            // radix sort, in tiles of per x 1024 keys
+  int passes, per;
+  int chunk, lanes;
+  bool wide;
   long long chunks;
   size_t keys[2], order[2], counts, parts, bytes;      // byte offsets of the workspace
 };
@@ -395,31 +420,32 @@ struct GradPlan {
 GradPlan plan_grad(int V, int D, long long N) {
   GradPlan p = {};
   p.rank = N <= kRankTokens;
-  p.tiles = (unsigned)((N + kSortTile - 1) / kSortTile);
+  // Small tiles while they leave CUs idle; a tile's counts are added by every other one, or by a launch of their own.
+  p.per = N <= (1 << 18) ? 4 : (N <= (1 << 21) ? 8 : 16);
+  p.tiles = (unsigned)((N + p.per * kSortThreads - 1) / (p.per * kSortThreads));
   p.passes = 0;
   if (!p.rank)
-    while (p.passes < 4 && ((uint64_t)V >> (8 * p.passes)) != 0) ++p.passes;       // (V itself is the key of ids that name no row)
+    while (p.passes < 4 && ((uint64_t)V >> (kDigitBits * p.passes)) != 0) ++p.passes;       // (V itself is the key of ids that name no row)
   // Chunks of 32 tokens; longer ones where that leaves more than 2^14 of them, so that a run of most tokens has few parts.
   p.chunk = 32;
   while ((N + p.chunk - 1) / p.chunk > (1 << 14)) p.chunk *= 2;
   p.chunks = (N + p.chunk - 1) / p.chunk;
   // Up to 64 columns a lane takes one; wider rows: eight a lane, sixteen-byte loads of 16-bit types.
-  p.vec = D <= 64 ? 1 : 8;
-  const int need = (D + p.vec - 1) / p.vec;
+  p.wide = D > 64;
   p.lanes = 1;
-  while (p.lanes < need && p.lanes < 64) p.lanes *= 2;
+  while (p.lanes < D && p.lanes < 64) p.lanes *= 2;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t was = at;
     at += (bytes + 255) / 256 * 256;
     return was;
   };
-  const size_t list = ((size_t)N + 8) * 4;
+  const size_t list = ((size_t)N + 16) * 4;
   for (int i = 0; i < (p.rank ? 1 : 2); ++i) {
     p.keys[i] = take(list);
     p.order[i] = take(list);
   }
-  p.counts = take(p.rank ? 0 : ((size_t)p.tiles + 1) * 256 * 4);
+  p.counts = take(p.rank ? 0 : ((size_t)p.tiles + 1) * kDigits * 4);
   p.parts = take((size_t)p.chunks * 2 * D * 4);
   p.bytes = at;
   return p;
@@ -478,18 +504,34 @@ kan_status run_lookup_grad(const LookupGradArgs& a, hipStream_t s) {
     if (st != KAN_OK) return st;
   } else {
     uint32_t* const counts = (uint32_t*)(ws + p.counts);
+    // The zeros are written beside the sort, whose launches leave most of the GPU idle: a share in each.
+    const int shares = 2 * p.passes;
+    const long long share = (fill / shares + 255) / 256 * 256;
     for (int pass = 0; pass < p.passes; ++pass) {
       const uint32_t* const kin = pass == 0 ? nullptr : keys[now];
       const uint32_t* const oin = pass == 0 ? nullptr : order[now];
       const int to = pass == 0 ? 0 : now ^ 1;
-      const unsigned fb = pass == 0 ? fill_blocks : 0;
+      unsigned char* part[2];
+      long long bytes[2];
+      unsigned fb[2];
+      for (int k = 0; k < 2; ++k) {
+        const long long from = std::min(fill, (2 * pass + k) * share);
+        part[k] = (unsigned char*)a.dtable + from;
+        bytes[k] = 2 * pass + k == shares - 1 ? fill - from : std::min(share, fill - from);
+        fb[k] = (unsigned)std::min(1024ll, (bytes[k] + 16 * kSortThreads - 1) / (16 * kSortThreads));
+      }
       st = run_named("kan_lookup_sort", s, [&] {
-        hipLaunchKernelGGL(kan_lookup_count_kernel, dim3(p.tiles + fb), dim3(kSortThreads), 0, s, a.ids, a.id_dtype, kin, a.N, (uint32_t)a.V,
-                           8 * pass, counts, p.tiles, (unsigned char*)a.dtable, fill);
+        hipLaunchKernelGGL(kan_lookup_count_kernel, dim3(p.tiles + fb[0]), dim3(kSortThreads), 0, s, a.ids, a.id_dtype, kin, a.N, (uint32_t)a.V,
+                           kDigitBits * pass, p.per, counts, p.tiles, part[0], bytes[0]);
         const bool scan = p.tiles > kInlineTiles;
-        if (scan) hipLaunchKernelGGL(kan_lookup_scan_kernel, dim3(256), dim3(256), 0, s, counts, p.tiles);
-        hipLaunchKernelGGL(kan_lookup_scatter_kernel, dim3(p.tiles), dim3(kSortThreads), 0, s, a.ids, a.id_dtype, kin, oin, a.N, (uint32_t)a.V,
-                           8 * pass, counts, p.tiles, (int)scan, keys[to], order[to]);
+        if (scan) hipLaunchKernelGGL(kan_lookup_scan_kernel, dim3(kDigits / 16), dim3(kSortThreads), 0, s, counts, p.tiles);
+        auto scatter = [&](auto per) {
+          hipLaunchKernelGGL((kan_lookup_scatter_kernel<decltype(per)::value>), dim3(p.tiles + fb[1]), dim3(kSortThreads), 0, s, a.ids, a.id_dtype, kin, oin,
+                             a.N, (uint32_t)a.V, kDigitBits * pass, counts, p.tiles, (int)scan, keys[to], order[to], part[1], bytes[1]);
+        };
+        if (p.per == 4) scatter(std::integral_constant<int, 4>{});
+        else if (p.per == 8) scatter(std::integral_constant<int, 8>{});
+        else scatter(std::integral_constant<int, 16>{});
         return hipGetLastError();
       });
       if (st != KAN_OK) return st;
@@ -497,15 +539,16 @@ kan_status run_lookup_grad(const LookupGradArgs& a, hipStream_t s) {
     }
   }
   SumArgs q = {order[now], keys[now], (float*)(ws + p.parts), a.N, (uint32_t)a.V, a.D, p.chunk, p.lanes, a.accumulate, a.scale};
-  const unsigned per_block = kThreads / p.lanes, col_tiles = (unsigned)((a.D + p.lanes * p.vec - 1) / (p.lanes * p.vec));
+  const int cols = p.lanes * (p.wide ? 8 : 1);
+  const unsigned per_block = kThreads / p.lanes, col_tiles = (unsigned)((a.D + cols - 1) / cols);
   const dim3 grid((unsigned)((p.chunks + per_block - 1) / per_block), col_tiles), join((unsigned)p.chunks, col_tiles);
   st = run_named("kan_lookup_sum", s, [&] {
     return with_float(a.dy_dtype, [&](auto i) {
       return with_float(a.dtable_dtype, [&](auto o) {
         typedef decltype(i) I;
         typedef decltype(o) O;
-        if (p.vec == 1) hipLaunchKernelGGL((kan_lookup_sum_kernel<I, O, 1>), grid, dim3(kThreads), 0, s, (const I*)a.dy, (O*)a.dtable, q);
-        else hipLaunchKernelGGL((kan_lookup_sum_kernel<I, O, 8>), grid, dim3(kThreads), 0, s, (const I*)a.dy, (O*)a.dtable, q);
+        if (p.wide) hipLaunchKernelGGL((kan_lookup_sum_kernel<I, O, true>), grid, dim3(kThreads), 0, s, (const I*)a.dy, (O*)a.dtable, q);
+        else hipLaunchKernelGGL((kan_lookup_sum_kernel<I, O, false>), grid, dim3(kThreads), 0, s, (const I*)a.dy, (O*)a.dtable, q);
         return hipGetLastError();
       });
     });
@@ -514,8 +557,8 @@ kan_status run_lookup_grad(const LookupGradArgs& a, hipStream_t s) {
   return run_named("kan_lookup_join", s, [&] {
     return with_float(a.dtable_dtype, [&](auto o) {
       typedef decltype(o) O;
-      if (p.vec == 1) hipLaunchKernelGGL((kan_lookup_join_kernel<O, 1>), join, dim3(kThreads), 0, s, (O*)a.dtable, q, p.chunks);
-      else hipLaunchKernelGGL((kan_lookup_join_kernel<O, 8>), join, dim3(kThreads), 0, s, (O*)a.dtable, q, p.chunks);
+      if (p.wide) hipLaunchKernelGGL((kan_lookup_join_kernel<O, true>), join, dim3(kJoinThreads), 0, s, (O*)a.dtable, q, p.chunks);
+      else hipLaunchKernelGGL((kan_lookup_join_kernel<O, false>), join, dim3(kJoinThreads), 0, s, (O*)a.dtable, q, p.chunks);
       return hipGetLastError();
     });
   });
