@@ -313,97 +313,132 @@ __global__ __launch_bounds__(kThreads) void kan_lookup_sum_kernel(const I* __res
     for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
     from_before = false;
   };
-  uint32_t key[8], at[8];
-#pragma unroll
-  for (int u = 0; u < 8; ++u) {       // (the arrays are padded: eight tokens behind the last chunk)
-    key[u] = a.keys[first + u];
-    at[u] = a.order[first + u];
-  }
-  for (long long p = first; p < end; p += 8) {
-    float v[8][VEC];
+  typedef I Raw __attribute__((ext_vector_type(VEC)));
+  const bool whole = c + VEC <= a.D;
+  uint32_t key[2][8];
+  Raw raw[2][8];
+  auto fetch = [&](long long p, int b) {       // (the arrays are padded: sixteen tokens behind the last one)
+    uint32_t at[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const bool live = p + u < end && key[u] < a.V;
+      key[b][u] = a.keys[p + u];
+      at[u] = a.order[p + u];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const bool live = p + u < end && key[b][u] < a.V;
       const I* const row = dy + (long long)(live ? at[u] : 0u) * a.D;
-      if constexpr (WIDE) load_cols(row, c, a.D, v[u]);
-      else v[u][0] = (float)row[c];
-    }
-    uint32_t key_next[8], at_next[8];
+      if (whole) {
+        __builtin_memcpy(&raw[b][u], row + c, sizeof(Raw));
+      } else {
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      key_next[u] = a.keys[p + 8 + u];
-      at_next[u] = a.order[p + 8 + u];
+        for (int i = 0; i < VEC; ++i) raw[b][u][i] = c + i < a.D ? row[c + i] : (I)0.f;
+      }
     }
+  };
+  auto take = [&](long long p, int b) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       if (p + u < end) {
-        if (key[u] != run) {
+        if (key[b][u] != run) {
           flush(false);
-          run = key[u];
+          run = key[b][u];
         }
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) sum[i] += v[u][i];
+        for (int i = 0; i < VEC; ++i) sum[i] += (float)raw[b][u][i];
       }
     }
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      key[u] = key_next[u];
-      at[u] = at_next[u];
-    }
+  };
+  fetch(first, 0);
+  for (long long p = first; p < end; p += 16) {
+    if (p + 8 < end) fetch(p + 8, 1);
+    take(p, 0);
+    if (p + 16 < end) fetch(p + 16, 0);
+    if (p + 8 < end) take(p + 8, 1);
   }
   flush(end < a.N && a.keys[end] == run);
 }
 
-// The run that begins in a chunk and goes on behind it: its parts, in order.  Groups of lanes take a share of the parts each.
-constexpr int kJoinThreads = 1024;
+// The runs that begin in a chunk and go on behind it: their parts, in order.  A group of lanes looks at a chunk and adds the
+// parts of a run that reaches up to kShort chunks further by itself; longer ones are left to all groups of the workgroup
+// together, a share of the parts each.
+constexpr int kJoinThreads = 1024, kShort = 16;
 template <class O, bool WIDE>
 __global__ __launch_bounds__(kJoinThreads) void kan_lookup_join_kernel(O* __restrict__ dtable, const SumArgs a, long long chunks) {
   constexpr int VEC = WIDE ? 8 : 1;
   __shared__ float sSum[kJoinThreads * VEC];
-  const int lanes = WIDE ? 64 : a.lanes;
-  const long long chunk = blockIdx.x;
-  const long long end = (chunk + 1) * a.chunk;
-  if (end >= a.N) return;
-  const long long first = chunk * a.chunk;
-  const uint32_t run = a.keys[end], last_in = a.keys[end - 1], first_in = a.keys[first], in_front = a.keys[max(first - 1, 0ll)];
-  if (run >= a.V || last_in != run) return;
-  if (first > 0 && first_in == run && in_front == run) return;       // it began further in front
-  // chunks behind this one that the run reaches
-  long long last = chunk + 1;
-  for (;;) {
-    const long long k = last + 1 + (threadIdx.x & 63);
-    const uint64_t on = __ballot(k < chunks && a.keys[min(k, chunks - 1) * a.chunk] == run);
-    const int n = on == ~0ull ? 64 : __ffsll((long long)~on) - 1;
-    last += n;
-    if (n < 64) break;
-  }
-  const int lane = threadIdx.x % lanes, group = threadIdx.x / lanes, groups = kJoinThreads / lanes;
+  __shared__ uint32_t sLong[kJoinThreads];        // chunks (of this workgroup) whose run is long
+  const int lanes = WIDE ? 64 : a.lanes, groups = kJoinThreads / lanes;
+  const int lane = threadIdx.x % lanes, group = threadIdx.x / lanes;
   const int c = (blockIdx.y * lanes + lane) * VEC;
-  const long long parts = last - chunk + 1, per = (parts + groups - 1) / groups;
-  const long long p0 = group * per, p1 = c < a.D ? min(parts, p0 + per) : 0;
+  const long long chunk = (long long)blockIdx.x * groups + group;
+  const long long first = min(chunk, chunks - 1) * a.chunk, end = first + a.chunk;
+  const uint32_t run = a.keys[min(end, a.N - 1)], last_in = a.keys[min(end, a.N) - 1], first_in = a.keys[first], in_front = a.keys[max(first - 1, 0ll)];
+  const bool mine = chunk < chunks && end < a.N && run < a.V && last_in == run && !(first > 0 && first_in == run && in_front == run);
+  int reach = 1;                  // chunks behind this one that the run is known to reach
+  for (int i = 0; i < kShort; i += lanes) {
+    const long long k = chunk + 2 + i + lane;
+    const uint64_t on = __ballot(mine && k < chunks && a.keys[min(k, chunks - 1) * a.chunk] == run) >> (threadIdx.x & 63 & ~(lanes - 1));
+    const int n = min(lanes, on == ~0ull ? 64 : __ffsll((long long)~on) - 1);
+    reach += reach == 1 + i ? n : 0;
+  }
+  const bool far = mine && reach > kShort;
+  if (lane == 0) sLong[group] = far ? 1u : 0u;
+  auto add = [&](float (&sum)[VEC], long long from, long long p0, long long p1) {
+    for (long long p = p0; p < p1; p += 8) {
+      float v[8][VEC];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const long long q = min(p + u, p1 - 1);
+        const float* const src = a.parts + (from + q) * 2 * a.D + (q == 0 ? a.D : 0);
+        if constexpr (WIDE) load_cols(src, c, a.D, v[u]);
+        else v[u][0] = src[c];
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) sum[i] += p + u < p1 ? v[u][i] : 0.f;
+    }
+  };
   float sum[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
-#pragma unroll 4
-  for (long long p = p0; p < p1; ++p) {
-    const float* const src = a.parts + (chunk + p) * 2 * a.D + (p == 0 ? a.D : 0);
-    float v[VEC];
-    if constexpr (WIDE) load_cols(src, c, a.D, v);
-    else v[0] = src[c];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) sum[i] += v[i];
+  if (mine && !far && c < a.D) {
+    add(sum, chunk, 0, reach + 1);
+    put<VEC>(dtable + (long long)run * a.D, c, a.D, sum, a);
   }
-#pragma unroll
-  for (int i = 0; i < VEC; ++i) sSum[(group * VEC + i) * lanes + lane] = sum[i];
   __syncthreads();
-  if (group != 0 || c >= a.D) return;
-  const int busy = (int)min((long long)groups, (parts + per - 1) / per);
+  for (int g = 0; g < groups; ++g) {
+    if (!sLong[g]) continue;
+    const long long from = (long long)blockIdx.x * groups + g;
+    const uint32_t key = a.keys[(from + 1) * a.chunk];
+    long long last = from + 1, past = chunks;       // the run reaches `last` and does not reach `past`
+    while (past - last > 1) {                       // a 64th of what is between them is left
+      const long long step = (past - last + 63) / 64, k = last + ((threadIdx.x & 63) + 1) * step;
+      const uint64_t on = __ballot(k < past && a.keys[min(k, chunks - 1) * a.chunk] == key);
+      const int n = __popcll(on);
+      past = min(past, last + (n + 1) * step);
+      last += n * step;
+    }
+    const long long parts = last - from + 1, per = (parts + groups - 1) / groups;
+    const long long p0 = group * per, p1 = c < a.D ? min(parts, p0 + per) : 0;
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
-  for (int g = 0; g < busy; ++g)
+    for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
+    add(sum, from, p0, p1);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) sum[i] += sSum[(g * VEC + i) * lanes + lane];
-  put<VEC>(dtable + (long long)run * a.D, c, a.D, sum, a);
+    for (int i = 0; i < VEC; ++i) sSum[(group * VEC + i) * lanes + lane] = sum[i];
+    __syncthreads();
+    if (group == 0 && c < a.D) {
+      const int busy = (int)min((long long)groups, (parts + per - 1) / per);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
+      for (int h = 0; h < busy; ++h)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) sum[i] += sSum[(h * VEC + i) * lanes + lane];
+      put<VEC>(dtable + (long long)key * a.D, c, a.D, sum, a);
+    }
+    __syncthreads();
+  }
 }
 
 // ---- plan of a gradient ----------------------------------------------------------------------------------------------
@@ -421,7 +456,7 @@ GradPlan plan_grad(int V, int D, long long N) {
   GradPlan p = {};
   p.rank = N <= kRankTokens;
   // Small tiles while they leave CUs idle; a tile's counts are added by every other one, or by a launch of their own.
-  p.per = N <= (1 << 18) ? 4 : (N <= (1 << 21) ? 8 : 16);
+  p.per = N <= (1 << 20) ? 4 : 16;
   p.tiles = (unsigned)((N + p.per * kSortThreads - 1) / (p.per * kSortThreads));
   p.passes = 0;
   if (!p.rank)
@@ -530,7 +565,6 @@ kan_status run_lookup_grad(const LookupGradArgs& a, hipStream_t s) {
                              a.N, (uint32_t)a.V, kDigitBits * pass, counts, p.tiles, (int)scan, keys[to], order[to], part[1], bytes[1]);
         };
         if (p.per == 4) scatter(std::integral_constant<int, 4>{});
-        else if (p.per == 8) scatter(std::integral_constant<int, 8>{});
         else scatter(std::integral_constant<int, 16>{});
         return hipGetLastError();
       });
@@ -541,7 +575,7 @@ kan_status run_lookup_grad(const LookupGradArgs& a, hipStream_t s) {
   SumArgs q = {order[now], keys[now], (float*)(ws + p.parts), a.N, (uint32_t)a.V, a.D, p.chunk, p.lanes, a.accumulate, a.scale};
   const int cols = p.lanes * (p.wide ? 8 : 1);
   const unsigned per_block = kThreads / p.lanes, col_tiles = (unsigned)((a.D + cols - 1) / cols);
-  const dim3 grid((unsigned)((p.chunks + per_block - 1) / per_block), col_tiles), join((unsigned)p.chunks, col_tiles);
+  const dim3 grid((unsigned)((p.chunks + per_block - 1) / per_block), col_tiles), join((unsigned)((p.chunks + kJoinThreads / p.lanes - 1) / (kJoinThreads / p.lanes)), col_tiles);
   st = run_named("kan_lookup_sum", s, [&] {
     return with_float(a.dy_dtype, [&](auto i) {
       return with_float(a.dtable_dtype, [&](auto o) {
