@@ -80,8 +80,7 @@ __device__ __forceinline__ void fill_zero(unsigned char* p, long long bytes, uns
 }
 
 __global__ __launch_bounds__(kRankThreads) void kan_lookup_rank_kernel(const void* __restrict__ ids, int id_dtype, int N, uint32_t V,
-                                                                       uint32_t* __restrict__ order, uint32_t* __restrict__ keys,
-                                                                       unsigned rank_blocks, unsigned char* fill, long long fill_bytes) {
+                                                                       uint2* __restrict__ sorted, unsigned rank_blocks, unsigned char* fill, long long fill_bytes) {
   __shared__ __attribute__((aligned(16))) uint32_t sKey[kRankTokens];
   __shared__ uint32_t sCount[16][64];
   if (blockIdx.x >= rank_blocks) {
@@ -110,13 +109,12 @@ __global__ __launch_bounds__(kRankThreads) void kan_lookup_rank_kernel(const voi
     uint32_t place = 0;
 #pragma unroll
     for (int w = 0; w < 16; ++w) place += sCount[w][lane];
-    order[place] = (uint32_t)mine;
-    keys[place] = key;
+    sorted[place] = make_uint2(key, (uint32_t)mine);
   }
 }
 
 // How often each digit occurs in each tile of `per` x 1024 keys.
-__global__ __launch_bounds__(kSortThreads) void kan_lookup_count_kernel(const void* __restrict__ ids, int id_dtype, const uint32_t* __restrict__ keys,
+__global__ __launch_bounds__(kSortThreads) void kan_lookup_count_kernel(const void* __restrict__ ids, int id_dtype, const uint2* __restrict__ pairs,
                                                                         long long N, uint32_t V, int shift, int per, uint32_t* __restrict__ counts,
                                                                         unsigned tiles, unsigned char* fill, long long fill_bytes) {
   __shared__ uint32_t sHist[kDigits];
@@ -130,7 +128,7 @@ __global__ __launch_bounds__(kSortThreads) void kan_lookup_count_kernel(const vo
 #pragma unroll 4
   for (int r = 0; r < per; ++r) {
     const long long n = first + r * kSortThreads + threadIdx.x;
-    if (n < N) atomicAdd(&sHist[((keys ? keys[n] : row_of(ids, id_dtype, n, V)) >> shift) & (kDigits - 1)], 1u);
+    if (n < N) atomicAdd(&sHist[((pairs ? pairs[n].x : row_of(ids, id_dtype, n, V)) >> shift) & (kDigits - 1)], 1u);
   }
   __syncthreads();
   if (threadIdx.x < kDigits) counts[(size_t)blockIdx.x * kDigits + threadIdx.x] = sHist[threadIdx.x];
@@ -157,29 +155,32 @@ __global__ __launch_bounds__(kSortThreads) void kan_lookup_scan_kernel(uint32_t*
   if (t == 63) counts[(size_t)tiles * kDigits + digit] = before;
 }
 
-// One pass of the sort: keys that agree in the digit keep their order.  A wave takes 64 PER keys in a row, 64 at a time: lanes
-// of equal digits find each other with a ballot per bit, a counter per wave and digit carries on.
+// One pass of the sort: pairs (key, position) that agree in the digit keep their order.  A wave takes 64 PER pairs in a row, 64
+// at a time: lanes of equal digits find each other with a ballot per bit, a counter per wave and digit carries on.  The tile is
+// sorted in LDS first, so that neighbouring lanes write neighbouring places.
 template <int PER>
-__global__ __launch_bounds__(kSortThreads) void kan_lookup_scatter_kernel(const void* __restrict__ ids, int id_dtype,
-                                                                          const uint32_t* __restrict__ keys_in, const uint32_t* __restrict__ order_in,
+__global__ __launch_bounds__(kSortThreads) void kan_lookup_scatter_kernel(const void* __restrict__ ids, int id_dtype, const uint2* __restrict__ in,
                                                                           long long N, uint32_t V, int shift, const uint32_t* __restrict__ counts,
-                                                                          unsigned tiles, int scanned, uint32_t* __restrict__ keys_out,
-                                                                          uint32_t* __restrict__ order_out, unsigned char* fill, long long fill_bytes) {
+                                                                          unsigned tiles, int scanned, uint2* __restrict__ out, unsigned char* fill,
+                                                                          long long fill_bytes) {
   __shared__ uint32_t sOff[16][kDigits];
   __shared__ uint32_t sPart[2][kDigits];
-  __shared__ uint32_t sWave[8];
+  __shared__ uint32_t sWave[2][8];
+  __shared__ uint32_t sTo[kDigits];
+  __shared__ uint2 sPair[PER * kSortThreads];
   if (blockIdx.x >= tiles) {
     fill_zero(fill, fill_bytes, blockIdx.x - tiles, gridDim.x - tiles);
     return;
   }
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (int i = tid; i < 16 * kDigits; i += kSortThreads) (&sOff[0][0])[i] = 0;
-  const long long first = (long long)blockIdx.x * PER * kSortThreads + wave * (64 * PER) + lane;
-  uint32_t key[PER], rank[PER];
+  const long long tile = (long long)blockIdx.x * PER * kSortThreads, first = tile + wave * (64 * PER) + lane;
+  uint2 pair[PER];
+  uint32_t rank[PER];
 #pragma unroll
   for (int r = 0; r < PER; ++r) {
     const long long n = first + r * 64;
-    key[r] = n < N ? (keys_in ? keys_in[n] : row_of(ids, id_dtype, n, V)) : 0u;
+    pair[r] = n >= N ? make_uint2(0u, 0u) : (in ? in[n] : make_uint2(row_of(ids, id_dtype, n, V), (uint32_t)n));
   }
   // keys of a digit in all tiles, and in those in front of this one
   uint32_t total = 0, before = 0;
@@ -208,7 +209,7 @@ __global__ __launch_bounds__(kSortThreads) void kan_lookup_scatter_kernel(const 
 #pragma unroll
   for (int r = 0; r < PER; ++r) {
     const bool live = first + r * 64 < N;
-    const uint32_t digit = (key[r] >> shift) & (kDigits - 1);
+    const uint32_t digit = (pair[r].x >> shift) & (kDigits - 1);
     uint64_t same = __ballot(live);
 #pragma unroll
     for (int b = 0; b < kDigitBits; ++b) {
@@ -221,22 +222,36 @@ __global__ __launch_bounds__(kSortThreads) void kan_lookup_scatter_kernel(const 
     if (live && (same >> lane) == 1ull) mine[digit] = rank[r] + 1;       // the last of its lanes
     __builtin_amdgcn_wave_barrier();
   }
-  uint32_t scan = 0;                  // keys of this digit and of smaller ones in its wave
+  __syncthreads();
+  uint32_t here = 0, scan_all = 0, scan_here = 0;      // keys of this digit in the tile; of it and of smaller ones in its wave
   if (tid < kDigits) {
     total += sPart[0][tid];
     before += sPart[1][tid];
-    scan = total;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) here += sOff[w][tid];
+    scan_all = total;
+    scan_here = here;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t o = __shfl_up(scan, d);
-      if (lane >= d) scan += o;
+      const uint32_t o = __shfl_up(scan_all, d), q = __shfl_up(scan_here, d);
+      if (lane >= d) {
+        scan_all += o;
+        scan_here += q;
+      }
     }
-    if (lane == 63) sWave[wave] = scan;
+    if (lane == 63) {
+      sWave[0][wave] = scan_all;
+      sWave[1][wave] = scan_here;
+    }
   }
   __syncthreads();
   if (tid < kDigits) {
-    uint32_t at = before + scan - total;
-    for (int w = 0; w < wave; ++w) at += sWave[w];
+    uint32_t all = before + scan_all - total, at = scan_here - here;
+    for (int w = 0; w < wave; ++w) {
+      all += sWave[0][w];
+      at += sWave[1][w];
+    }
+    sTo[tid] = all - at;
 #pragma unroll
     for (int w = 0; w < 16; ++w) {
       const uint32_t c = sOff[w][tid];
@@ -246,19 +261,23 @@ __global__ __launch_bounds__(kSortThreads) void kan_lookup_scatter_kernel(const 
   }
   __syncthreads();
 #pragma unroll
+  for (int r = 0; r < PER; ++r)
+    if (first + r * 64 < N) sPair[sOff[wave][(pair[r].x >> shift) & (kDigits - 1)] + rank[r]] = pair[r];
+  __syncthreads();
+  const int live = (int)min((long long)PER * kSortThreads, N - tile);
+#pragma unroll
   for (int r = 0; r < PER; ++r) {
-    const long long n = first + r * 64;
-    if (n < N) {
-      const uint32_t to = sOff[wave][(key[r] >> shift) & (kDigits - 1)] + rank[r];
-      keys_out[to] = key[r];
-      order_out[to] = order_in ? order_in[n] : (uint32_t)n;
+    const int i = r * kSortThreads + tid;
+    if (i < live) {
+      const uint2 p = sPair[i];
+      out[sTo[(p.x >> shift) & (kDigits - 1)] + (uint32_t)i] = p;
     }
   }
 }
 
 // ---- sums over runs of the sorted tokens ----------------------------------------------------------------------------
 struct SumArgs {
-  const uint32_t *order, *keys;
+  const uint2* sorted;       // (row, token)
   float* parts;              // [chunk][2][D]: what the chunk has of the run that began in front of it, and of the one that
                              // goes on behind it (a run that does both: the first)
   long long N;
@@ -296,8 +315,8 @@ __global__ __launch_bounds__(kThreads) void kan_lookup_sum_kernel(const I* __res
   float sum[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
-  uint32_t run = a.keys[first];
-  bool from_before = first > 0 && a.keys[first - 1] == run;
+  uint32_t run = a.sorted[first].x;
+  bool from_before = first > 0 && a.sorted[first - 1].x == run;
   float* const parts = a.parts + chunk * 2 * a.D;
   auto flush = [&](bool goes_on) {
     if (run < a.V) {
@@ -321,8 +340,9 @@ __global__ __launch_bounds__(kThreads) void kan_lookup_sum_kernel(const I* __res
     uint32_t at[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      key[b][u] = a.keys[p + u];
-      at[u] = a.order[p + u];
+      const uint2 t = a.sorted[p + u];
+      key[b][u] = t.x;
+      at[u] = t.y;
     }
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
@@ -356,7 +376,7 @@ __global__ __launch_bounds__(kThreads) void kan_lookup_sum_kernel(const I* __res
     if (p + 16 < end) fetch(p + 16, 0);
     if (p + 8 < end) take(p + 8, 1);
   }
-  flush(end < a.N && a.keys[end] == run);
+  flush(end < a.N && a.sorted[end].x == run);
 }
 
 // The runs that begin in a chunk and go on behind it: their parts, in order.  A group of lanes looks at a chunk and adds the
@@ -373,12 +393,12 @@ __global__ __launch_bounds__(kJoinThreads) void kan_lookup_join_kernel(O* __rest
   const int c = (blockIdx.y * lanes + lane) * VEC;
   const long long chunk = (long long)blockIdx.x * groups + group;
   const long long first = min(chunk, chunks - 1) * a.chunk, end = first + a.chunk;
-  const uint32_t run = a.keys[min(end, a.N - 1)], last_in = a.keys[min(end, a.N) - 1], first_in = a.keys[first], in_front = a.keys[max(first - 1, 0ll)];
+  const uint32_t run = a.sorted[min(end, a.N - 1)].x, last_in = a.sorted[min(end, a.N) - 1].x, first_in = a.sorted[first].x, in_front = a.sorted[max(first - 1, 0ll)].x;
   const bool mine = chunk < chunks && end < a.N && run < a.V && last_in == run && !(first > 0 && first_in == run && in_front == run);
   int reach = 1;                  // chunks behind this one that the run is known to reach
   for (int i = 0; i < kShort; i += lanes) {
     const long long k = chunk + 2 + i + lane;
-    const uint64_t on = __ballot(mine && k < chunks && a.keys[min(k, chunks - 1) * a.chunk] == run) >> (threadIdx.x & 63 & ~(lanes - 1));
+    const uint64_t on = __ballot(mine && k < chunks && a.sorted[min(k, chunks - 1) * a.chunk].x == run) >> (threadIdx.x & 63 & ~(lanes - 1));
     const int n = min(lanes, on == ~0ull ? 64 : __ffsll((long long)~on) - 1);
     reach += reach == 1 + i ? n : 0;
   }
@@ -411,11 +431,11 @@ __global__ __launch_bounds__(kJoinThreads) void kan_lookup_join_kernel(O* __rest
   for (int g = 0; g < groups; ++g) {
     if (!sLong[g]) continue;
     const long long from = (long long)blockIdx.x * groups + g;
-    const uint32_t key = a.keys[(from + 1) * a.chunk];
+    const uint32_t key = a.sorted[(from + 1) * a.chunk].x;
     long long last = from + 1, past = chunks;       // the run reaches `last` and does not reach `past`
     while (past - last > 1) {                       // a 64th of what is between them is left
       const long long step = (past - last + 63) / 64, k = last + ((threadIdx.x & 63) + 1) * step;
-      const uint64_t on = __ballot(k < past && a.keys[min(k, chunks - 1) * a.chunk] == key);
+      const uint64_t on = __ballot(k < past && a.sorted[min(k, chunks - 1) * a.chunk].x == key);
       const int n = __popcll(on);
       past = min(past, last + (n + 1) * step);
       last += n * step;
@@ -449,20 +469,21 @@ struct GradPlan {
   int chunk, lanes;
   bool wide;
   long long chunks;
-  size_t keys[2], order[2], counts, parts, bytes;      // byte offsets of the workspace
+  size_t sorted[2], counts, parts, bytes;      // byte offsets of the workspace
 };
 
 GradPlan plan_grad(int V, int D, long long N) {
   GradPlan p = {};
   p.rank = N <= kRankTokens;
   // Small tiles while they leave CUs idle; a tile's counts are added by every other one, or by a launch of their own.
-  p.per = N <= (1 << 20) ? 4 : 16;
+  p.per = N <= (1 << 20) ? 4 : 8;
   p.tiles = (unsigned)((N + p.per * kSortThreads - 1) / (p.per * kSortThreads));
   p.passes = 0;
   if (!p.rank)
     while (p.passes < 4 && ((uint64_t)V >> (kDigitBits * p.passes)) != 0) ++p.passes;       // (V itself is the key of ids that name no row)
-  // Chunks of 32 tokens; longer ones where that leaves more than 2^14 of them, so that a run of most tokens has few parts.
-  p.chunk = 32;
+  // Chunks of 32 tokens; of 64 where that leaves 2048 waves busy (fewer rows are written in parts: 66 against 70 us for 16,384
+  // tokens x 4096); longer ones where there would be more than 2^14 of them, so that a run of most tokens has few parts.
+  p.chunk = N / 64 * ((D + 511) / 512) >= 2048 ? 64 : 32;
   while ((N + p.chunk - 1) / p.chunk > (1 << 14)) p.chunk *= 2;
   p.chunks = (N + p.chunk - 1) / p.chunk;
   // Up to 64 columns a lane takes one; wider rows: eight a lane, sixteen-byte loads of 16-bit types.
@@ -475,11 +496,8 @@ GradPlan plan_grad(int V, int D, long long N) {
     at += (bytes + 255) / 256 * 256;
     return was;
   };
-  const size_t list = ((size_t)N + 16) * 4;
-  for (int i = 0; i < (p.rank ? 1 : 2); ++i) {
-    p.keys[i] = take(list);
-    p.order[i] = take(list);
-  }
+  const size_t list = ((size_t)N + 16) * 8;
+  for (int i = 0; i < (p.rank ? 1 : 2); ++i) p.sorted[i] = take(list);
   p.counts = take(p.rank ? 0 : ((size_t)p.tiles + 1) * kDigits * 4);
   p.parts = take((size_t)p.chunks * 2 * D * 4);
   p.bytes = at;
@@ -519,21 +537,20 @@ kan_status run_lookup_grad(const LookupGradArgs& a, hipStream_t s) {
     if (!fill) return KAN_OK;
     return run_named("kan_lookup_fill", s, [&] {
       hipLaunchKernelGGL(kan_lookup_rank_kernel, dim3(fill_blocks), dim3(kRankThreads), 0, s, a.ids, a.id_dtype, 0, (uint32_t)a.V,
-                         (uint32_t*)nullptr, (uint32_t*)nullptr, 0u, (unsigned char*)a.dtable, fill);
+                         (uint2*)nullptr, 0u, (unsigned char*)a.dtable, fill);
       return hipGetLastError();
     });
   }
   const GradPlan p = plan_grad(a.V, a.D, a.N);
   unsigned char* const ws = (unsigned char*)a.ws;
-  uint32_t* keys[2] = {(uint32_t*)(ws + p.keys[0]), (uint32_t*)(ws + p.keys[1])};
-  uint32_t* order[2] = {(uint32_t*)(ws + p.order[0]), (uint32_t*)(ws + p.order[1])};
+  uint2* const sorted[2] = {(uint2*)(ws + p.sorted[0]), (uint2*)(ws + p.sorted[1])};
   int now = 0;
   kan_status st;
   if (p.rank) {
     const unsigned blocks = (unsigned)((a.N + 63) / 64);
     st = run_named("kan_lookup_rank", s, [&] {
       hipLaunchKernelGGL(kan_lookup_rank_kernel, dim3(blocks + fill_blocks), dim3(kRankThreads), 0, s, a.ids, a.id_dtype, (int)a.N,
-                         (uint32_t)a.V, order[0], keys[0], blocks, (unsigned char*)a.dtable, fill);
+                         (uint32_t)a.V, sorted[0], blocks, (unsigned char*)a.dtable, fill);
       return hipGetLastError();
     });
     if (st != KAN_OK) return st;
@@ -543,8 +560,7 @@ kan_status run_lookup_grad(const LookupGradArgs& a, hipStream_t s) {
     const int shares = 2 * p.passes;
     const long long share = (fill / shares + 255) / 256 * 256;
     for (int pass = 0; pass < p.passes; ++pass) {
-      const uint32_t* const kin = pass == 0 ? nullptr : keys[now];
-      const uint32_t* const oin = pass == 0 ? nullptr : order[now];
+      const uint2* const in = pass == 0 ? nullptr : sorted[now];
       const int to = pass == 0 ? 0 : now ^ 1;
       unsigned char* part[2];
       long long bytes[2];
@@ -556,23 +572,23 @@ kan_status run_lookup_grad(const LookupGradArgs& a, hipStream_t s) {
         fb[k] = (unsigned)std::min(1024ll, (bytes[k] + 16 * kSortThreads - 1) / (16 * kSortThreads));
       }
       st = run_named("kan_lookup_sort", s, [&] {
-        hipLaunchKernelGGL(kan_lookup_count_kernel, dim3(p.tiles + fb[0]), dim3(kSortThreads), 0, s, a.ids, a.id_dtype, kin, a.N, (uint32_t)a.V,
+        hipLaunchKernelGGL(kan_lookup_count_kernel, dim3(p.tiles + fb[0]), dim3(kSortThreads), 0, s, a.ids, a.id_dtype, in, a.N, (uint32_t)a.V,
                            kDigitBits * pass, p.per, counts, p.tiles, part[0], bytes[0]);
         const bool scan = p.tiles > kInlineTiles;
         if (scan) hipLaunchKernelGGL(kan_lookup_scan_kernel, dim3(kDigits / 16), dim3(kSortThreads), 0, s, counts, p.tiles);
         auto scatter = [&](auto per) {
-          hipLaunchKernelGGL((kan_lookup_scatter_kernel<decltype(per)::value>), dim3(p.tiles + fb[1]), dim3(kSortThreads), 0, s, a.ids, a.id_dtype, kin, oin,
-                             a.N, (uint32_t)a.V, kDigitBits * pass, counts, p.tiles, (int)scan, keys[to], order[to], part[1], bytes[1]);
+          hipLaunchKernelGGL((kan_lookup_scatter_kernel<decltype(per)::value>), dim3(p.tiles + fb[1]), dim3(kSortThreads), 0, s, a.ids, a.id_dtype, in,
+                             a.N, (uint32_t)a.V, kDigitBits * pass, counts, p.tiles, (int)scan, sorted[to], part[1], bytes[1]);
         };
         if (p.per == 4) scatter(std::integral_constant<int, 4>{});
-        else scatter(std::integral_constant<int, 16>{});
+        else scatter(std::integral_constant<int, 8>{});
         return hipGetLastError();
       });
       if (st != KAN_OK) return st;
       now = to;
     }
   }
-  SumArgs q = {order[now], keys[now], (float*)(ws + p.parts), a.N, (uint32_t)a.V, a.D, p.chunk, p.lanes, a.accumulate, a.scale};
+  SumArgs q = {sorted[now], (float*)(ws + p.parts), a.N, (uint32_t)a.V, a.D, p.chunk, p.lanes, a.accumulate, a.scale};
   const int cols = p.lanes * (p.wide ? 8 : 1);
   const unsigned per_block = kThreads / p.lanes, col_tiles = (unsigned)((a.D + cols - 1) / cols);
   const dim3 grid((unsigned)((p.chunks + per_block - 1) / per_block), col_tiles), join((unsigned)((p.chunks + kJoinThreads / p.lanes - 1) / (kJoinThreads / p.lanes)), col_tiles);
