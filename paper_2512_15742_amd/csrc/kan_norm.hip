@@ -9,7 +9,8 @@
 //   dw_before = sum du y ry,   dw_after = sum scale s gy m     (over the tokens)
 //
 // Bound by the bytes of the rows: each is read once, a row stays in the registers of one to sixteen waves, eight columns a
-// lane at a time.  Norms, means and the sums of the weights' gradients are fp32.  The u of the forward pass is formed from
+// lane at a time (8192 rows of 2048 in bf16 with fp32 blocks and gates forward 53 us, 5.0 TB/s; of 4096 in bf16 backward 113 us,
+// 4.7 TB/s; a large copy reaches 5.1).  Norms, means and the sums of the weights' gradients are fp32.  The u of the forward pass is formed from
 // the fp32 y, not from its rounded copy.  Backward: up to 512 groups of waves take rows in turn and keep the sums of their
 // rows' weight gradients in registers; a second launch adds the groups' sums in a fixed order.
 #include <algorithm>
@@ -22,7 +23,7 @@ namespace {
 
 constexpr int kMaxGroups = 512;         // groups of waves of a backward launch, each with a partial sum of the weights' gradients
 constexpr int kMaxBlocks = 1 << 20;     // workgroups of a forward launch: they take rows in turn
-constexpr int kReduceThreads = 1024;    // 64 columns, 16 shares of the groups
+constexpr int kReduceThreads = 1024;    // 16 columns, 64 shares of the groups
 
 __device__ __forceinline__ void load_weight(const void* w, int dtype, int c, int D, float (&out)[8]) {
   if (!w) {
@@ -37,7 +38,8 @@ __device__ __forceinline__ void load_weight(const void* w, int dtype, int c, int
   }
 }
 
-// Sums of K values over the W waves of a row, the same in every lane.
+// Sums of K values over the W waves of a row, the same in every lane.  The scratch has to be another one than that of the call
+// before: the barrier here is then the only one, since nobody passes the next call's before everybody has read this one's.
 template <int W, int K>
 __device__ __forceinline__ void row_sums(float (&v)[K], float (*scratch)[K]) {
 #pragma unroll
@@ -46,7 +48,6 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float (*scratch)[K]) {
     for (int d = 32; d >= 1; d >>= 1) v[k] += __shfl_xor(v[k], d);
   if constexpr (W > 1) {
     const int wave = threadIdx.x >> 6;
-    __syncthreads();                 // (the scratch of the row before has been read)
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
       for (int k = 0; k < K; ++k) scratch[wave][k] = v[k];
@@ -66,7 +67,7 @@ __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf
 // W waves a row, W == 1: four rows a workgroup.
 template <class S, class B, int W, int P>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_kernel(const NormArgs a) {
-  __shared__ float sSum[W][1];
+  __shared__ float sSum[2][W][1];
   const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x;
   const int D = a.D;
   const float inv = 1.f / (float)D;
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_kernel(const N
       for (int p = 0; p < P; ++p)
   #pragma unroll
         for (int i = 0; i < 8; ++i) ss[0] += v[p][i] * v[p][i];
-      row_sums<W, 1>(ss, sSum);
+      row_sums<W, 1>(ss, sSum[0]);
       const float r = a.scale * rsqrtf(ss[0] * inv + a.eps);
   #pragma unroll
       for (int p = 0; p < P; ++p) {
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_kernel(const N
       for (int p = 0; p < P; ++p)
   #pragma unroll
         for (int i = 0; i < 8; ++i) ss[0] += x[p][i] * x[p][i];
-      row_sums<W, 1>(ss, sSum);
+      row_sums<W, 1>(ss, sSum[1]);
       const float r = rsqrtf(ss[0] * inv + a.eps);
   #pragma unroll
       for (int p = 0; p < P; ++p) {
@@ -134,100 +135,126 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_kernel(const N
   }
 }
 
+// Eight columns of a row as they lie in memory; zeros past its end.
+template <class T>
+struct Raw {
+  typedef T V8 __attribute__((ext_vector_type(8)));
+  V8 v;
+  __device__ __forceinline__ void load(const void* row, int c, int D) {
+    const T* const p = (const T*)row + c;
+    if (c + 8 <= D) {
+      __builtin_memcpy(&v, p, sizeof(v));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = c + i < D ? p[i] : (T)0.f;
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (T)0.f;
+  }
+  __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
+};
+
+// W waves a row, weights and their sums in registers: 128 of them where a lane has one group of columns, so that two rows
+// share a CU and the loads of one run beside the sums of the other (8192 rows of 4096 in bf16: 113 us; the next row fetched
+// ahead, with 155 registers and one row a CU, 122).
 template <class S, class B, int W, int P>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_grad_kernel(const NormArgs a, int groups) {
-  __shared__ float sSum[W][3];
-  __shared__ float sSum1[W][1];
-  const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x;
-  const int group = W == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
-  if (group >= groups) return;
-  const int D = a.D;
+__global__ __launch_bounds__(64 * W, P == 1 ? 4 : 1) void kan_norm_grad_kernel(const NormArgs a, int groups) {
+  __shared__ float sSum[2][W][3];
+  __shared__ float sSum1[2][W][1];
+  const int t = threadIdx.x, group = blockIdx.x, D = a.D;
   const float inv = 1.f / (float)D;
-  float sum1[P][8], sum2[P][8];
+  float sum1[P][8], sum2[P][8], w1[P][8], w2[P][8];
 #pragma unroll
-  for (int p = 0; p < P; ++p)
+  for (int p = 0; p < P; ++p) {
+    const int c = (p * 64 * W + t) * 8;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum1[p][i] = sum2[p][i] = 0.f;
-  for (long long n = group; n < a.N; n += groups) {
-    float y[P][8], gy[P][8], du[P][8], v[P][8], g[P][8];
+    for (int i = 0; i < 8; ++i) sum1[p][i] = sum2[p][i] = w1[p][i] = w2[p][i] = 0.f;
+    if (c < D) {
+      if (a.du) load_weight(a.w_before, a.weight_dtype, c, D, w1[p]);
+      if (a.v) load_weight(a.w_after, a.weight_dtype, c, D, w2[p]);
+      if (c + 8 > D)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (c + i >= D) w1[p][i] = w2[p][i] = 0.f;
+    }
+  }
+  struct Row {
+    Raw<S> y[P], dy[P];
+    Raw<B> du[P], v[P], g[P];
+  };
+  auto load = [&](long long n, Row& r) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = (p * 64 * W + t) * 8;
+      r.y[p].clear(), r.dy[p].clear(), r.du[p].clear(), r.v[p].clear(), r.g[p].clear();
+      if (c < D) {
+        if (a.du) {
+          r.y[p].load((const S*)a.x + n * D, c, D);
+          r.du[p].load((const B*)a.du + n * D, c, D);
+        }
+        if (a.dy) r.dy[p].load((const S*)a.dy + n * D, c, D);
+        if (a.v) r.v[p].load((const B*)a.v + n * D, c, D);
+        if (a.gate) r.g[p].load((const B*)a.gate + n * D, c, D);
+      }
+    }
+  };
+  auto work = [&](long long n, const Row& r, int odd) {
     float ss[3] = {0.f, 0.f, 0.f};
 #pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        ss[0] += r.y[p][i] * r.y[p][i];
+        ss[1] += r.du[p][i] * w1[p][i] * r.y[p][i];
+        ss[2] += r.v[p][i] * r.v[p][i];
+      }
+    row_sums<W, 3>(ss, sSum[odd]);
+    const float ry = rsqrtf(ss[0] * inv + a.eps), rv = rsqrtf(ss[2] * inv + a.eps), mean = ss[1] * ry * inv;
+    float sq[1] = {0.f}, q[P][8];
+#pragma unroll
     for (int p = 0; p < P; ++p) {
       const int c = (p * 64 * W + t) * 8;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[p][i] = gy[p][i] = du[p][i] = v[p][i] = g[p][i] = 0.f;
-      if (c < D) {
+      for (int i = 0; i < 8; ++i) {
+        q[p][i] = r.dy[p][i];
         if (a.du) {
-          load_cols((const S*)a.x + n * D, c, D, y[p]);
-          load_cols((const B*)a.du + n * D, c, D, du[p]);
-        }
-        if (a.dy) load_cols((const S*)a.dy + n * D, c, D, gy[p]);
-        if (a.v) {
-          load_cols((const B*)a.v + n * D, c, D, v[p]);
-          if (a.gate) load_cols((const B*)a.gate + n * D, c, D, g[p]);
+          const float hat = r.y[p][i] * ry;
+          sum1[p][i] += r.du[p][i] * hat;
+          q[p][i] += ry * (r.du[p][i] * w1[p][i] - hat * mean);
         }
       }
-    }
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int c = (p * 64 * W + t) * 8;
-      if (c < D) {
-        float w[8];
-        load_weight(a.w_before, a.weight_dtype, c, D, w);
+      if (c < D) store_cols((S*)a.dx + n * D, c, D, q[p]);
+      if (a.v) {
+        float dg[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          ss[0] += y[p][i] * y[p][i];
-          ss[1] += c + i < D ? du[p][i] * w[i] * y[p][i] : 0.f;
-          ss[2] += v[p][i] * v[p][i];
+          const float s = a.gate ? sigmoid(r.g[p][i]) : 1.f, m = r.v[p][i] * rv, e = a.scale * q[p][i];
+          sum2[p][i] += s * e * m;
+          dg[i] = e * (w2[p][i] * m) * (s * (1.f - s));
+          q[p][i] = s * e * w2[p][i];
+          sq[0] += c + i < D ? q[p][i] * m : 0.f;
         }
-      }
-    }
-    row_sums<W, 3>(ss, sSum);
-    const float ry = rsqrtf(ss[0] * inv + a.eps), rv = rsqrtf(ss[2] * inv + a.eps), mean = ss[1] * ry * inv;
-    float sq[1] = {0.f};
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int c = (p * 64 * W + t) * 8;
-      if (c < D) {
-        float w[8];
-        if (a.du) {
-          load_weight(a.w_before, a.weight_dtype, c, D, w);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float hat = y[p][i] * ry;
-            sum1[p][i] += du[p][i] * hat;
-            gy[p][i] += ry * (du[p][i] * w[i] - hat * mean);
-          }
-        }
-        store_cols((S*)a.dx + n * D, c, D, gy[p]);
-        if (a.v) {
-          load_weight(a.w_after, a.weight_dtype, c, D, w);
-          float dg[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float s = a.gate ? sigmoid(g[p][i]) : 1.f, m = v[p][i] * rv, e = a.scale * gy[p][i];
-            sum2[p][i] += s * e * m;
-            dg[i] = e * (w[i] * m) * (s * (1.f - s));
-            gy[p][i] = s * e * w[i];                       // q from here on
-            sq[0] += c + i < D ? gy[p][i] * m : 0.f;
-          }
-          if (a.gate) store_cols((B*)a.dgate + n * D, c, D, dg);
-        }
+        if (a.gate && c < D) store_cols((B*)a.dgate + n * D, c, D, dg);
       }
     }
     if (a.v) {
-      row_sums<W, 1>(sq, sSum1);
+      row_sums<W, 1>(sq, sSum1[odd]);
       const float qm = sq[0] * inv;
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         const int c = (p * 64 * W + t) * 8;
-        if (c < D) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) gy[p][i] = rv * (gy[p][i] - v[p][i] * rv * qm);
-          store_cols((B*)a.dv + n * D, c, D, gy[p]);
-        }
+        for (int i = 0; i < 8; ++i) q[p][i] = rv * (q[p][i] - r.v[p][i] * rv * qm);
+        if (c < D) store_cols((B*)a.dv + n * D, c, D, q[p]);
       }
     }
+  };
+  for (long long n = group, odd = 0; n < a.N; n += groups, odd ^= 1) {
+    Row r;
+    load(n, r);
+    work(n, r, (int)odd);
   }
   // sums[0]: w_before, then w_after, as far as they are asked for
   float* dst = a.partial + (long long)group * D;
@@ -241,29 +268,28 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_grad_kernel(co
   }
 }
 
+// 16 columns a workgroup, 64 shares of the groups.
 __global__ __launch_bounds__(kReduceThreads) void kan_norm_reduce_kernel(const float* __restrict__ partial, int groups, int D, void* first, void* second,
                                                                          int dtype) {
-  __shared__ float sSum[16][64];
-  const int lane = threadIdx.x & 63, share = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  __shared__ float sSum[64][17];
+  const int lane = threadIdx.x & 15, share = threadIdx.x >> 4, c = blockIdx.x * 16 + lane;
   const float* const src = partial + (long long)blockIdx.y * groups * D;
   float s = 0.f;
   if (c < D) {
-    int r = share;
-    for (; r + 7 * 16 < groups; r += 8 * 16) {
+    for (int r = share; r < groups; r += 8 * 64) {
       float v[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = src[(long long)(r + u * 16) * D + c];
+      for (int u = 0; u < 8; ++u) v[u] = r + u * 64 < groups ? src[(long long)(r + u * 64) * D + c] : 0.f;
 #pragma unroll
       for (int u = 0; u < 8; ++u) s += v[u];
     }
-    for (; r < groups; r += 16) s += src[(long long)r * D + c];
   }
   sSum[share][lane] = s;
   __syncthreads();
   if (share == 0 && c < D) {
     s = 0.f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s += sSum[k][lane];
+    for (int k = 0; k < 64; ++k) s += sSum[k][lane];
     void* const out = blockIdx.y == 0 ? first : second;
     if (dtype == KAN_F32) ((float*)out)[c] = s;
     else if (dtype == KAN_F16) ((f16*)out)[c] = (f16)s;
@@ -271,14 +297,20 @@ __global__ __launch_bounds__(kReduceThreads) void kan_norm_reduce_kernel(const f
   }
 }
 
-// f(W, P): waves per row and groups of eight columns a lane.
-template <class F>
+// f(W, P): waves per row and groups of eight columns a lane.  Backward a row takes more registers, and more waves.
+template <bool GRAD, class F>
 hipError_t with_shape(int D, F&& f) {
 #define KAN_SHAPE(W, P) if (D <= 512 * W * P) return f(std::integral_constant<int, W>{}, std::integral_constant<int, P>{})
   KAN_SHAPE(1, 1);
-  KAN_SHAPE(1, 2);
-  KAN_SHAPE(4, 1);
-  KAN_SHAPE(4, 2);
+  if constexpr (GRAD) {
+    KAN_SHAPE(2, 1);
+    KAN_SHAPE(4, 1);
+    KAN_SHAPE(8, 1);
+  } else {
+    KAN_SHAPE(1, 2);
+    KAN_SHAPE(4, 1);
+    KAN_SHAPE(4, 2);
+  }
   KAN_SHAPE(8, 2);
   return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
 #undef KAN_SHAPE
@@ -301,7 +333,7 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
   return with_types(a.stream_dtype, a.block_dtype, [&](auto st, auto bl) {
     typedef decltype(st) S;
     typedef decltype(bl) B;
-    return with_shape(a.D, [&](auto w, auto p) {
+    return with_shape<false>(a.D, [&](auto w, auto p) {
       constexpr int W = decltype(w)::value, P = decltype(p)::value;
       const long long blocks = std::min(W == 1 ? (a.N + 3) / 4 : a.N, (long long)kMaxBlocks);
       hipLaunchKernelGGL((kan_norm_kernel<S, B, W, P>), dim3((unsigned)blocks), dim3(W == 1 ? 256 : 64 * W), 0, s, a);
@@ -321,10 +353,9 @@ kan_status run_norm_grad(const NormArgs& a, hipStream_t s) {
     return with_types(a.stream_dtype, a.block_dtype, [&](auto str, auto bl) {
       typedef decltype(str) S;
       typedef decltype(bl) B;
-      return with_shape(a.D, [&](auto w, auto p) {
+      return with_shape<true>(a.D, [&](auto w, auto p) {
         constexpr int W = decltype(w)::value, P = decltype(p)::value;
-        const int blocks = W == 1 ? (groups + 3) / 4 : groups;
-        hipLaunchKernelGGL((kan_norm_grad_kernel<S, B, W, P>), dim3(blocks), dim3(W == 1 ? 256 : 64 * W), 0, s, a, groups);
+        hipLaunchKernelGGL((kan_norm_grad_kernel<S, B, W, P>), dim3(groups), dim3(64 * W), 0, s, a, groups);
         return hipGetLastError();
       });
     });
@@ -332,7 +363,7 @@ kan_status run_norm_grad(const NormArgs& a, hipStream_t s) {
   const int sums = (a.dw_before ? 1 : 0) + (a.dw_after ? 1 : 0);
   if (st != KAN_OK || sums == 0) return st;
   return run_named("kan_norm_reduce", s, [&] {
-    hipLaunchKernelGGL(kan_norm_reduce_kernel, dim3((a.D + 63) / 64, sums), dim3(kReduceThreads), 0, s, a.partial, groups, a.D,
+    hipLaunchKernelGGL(kan_norm_reduce_kernel, dim3((a.D + 15) / 16, sums), dim3(kReduceThreads), 0, s, a.partial, groups, a.D,
                        a.dw_before ? a.dw_before : a.dw_after, a.dw_after, a.weight_dtype);
     return hipGetLastError();
   });
