@@ -30,7 +30,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kStep = 32;               // products along the contraction per step
-constexpr int kTile = 256;              // results of a workgroup in either direction
 constexpr int kSlots = 4;               // steps whose operands LDS holds
 constexpr int kVocabStep = 256;         // pieces of the table are multiples of it
 constexpr long long kPackBytes = 256ll << 20, kPieceBytes = 512ll << 20;
@@ -64,10 +63,8 @@ struct ProductArgs {
   // kStats, kGradS: m = rows of the table from `v0` on, n = tokens
   int v0, V;
   float scale;
-  const void* targets;       // kGradS: 32-bit rows of the table
-  int id_dtype;
   float2* stats;             // [tile of the table][tokens]
-  float* target_z;
+  const int* targets;        // kGradS
   const float *lse, *weight;
   void* ds;                  // [part][n][ds_stride]
   long long ds_stride, ds_part;
@@ -218,8 +215,8 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
   const int n_here = EPI != kGradTable && g.count ? min(g.n, *g.count) : g.n, k_here = EPI == kGradTable && g.count ? min(g.k, *g.count) : g.k;
   // Runs of consecutive work items per XCD; eight tiles of n by as many of m as it has workgroups.
   int mt, nt, split;
+  const unsigned nmt = (unsigned)(g.m + BM - 1) / BM, nnt = (unsigned)(n_here + BN - 1) / BN, tiles = nmt * nnt, W = tiles * (unsigned)g.splits;
   {
-    const unsigned nmt = (unsigned)(g.m + BM - 1) / BM, nnt = (unsigned)(n_here + BN - 1) / BN, tiles = nmt * nnt, W = tiles * (unsigned)g.splits;
     const unsigned L = blockIdx.x, xcd = L & 7u, q = W >> 3, r = W & 7u;
     if (L >= W) return;
     const unsigned work = xcd * q + min(xcd, r) + (L >> 3), item = work % tiles;
@@ -239,7 +236,10 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sRing;
 
   // The next copies: product of parts, k, slot.  Past the last one everything is behind the buffers' ends.
-  int cq = g.parts == 1 ? 0 : s0 / max(ksteps, 1), ck = (s0 - cq * ksteps) * kStep, cs = 0;
+  // With one tile of n every row of the table is read by one workgroup: each begins at another k, since rows of 2^n bytes in step
+  // would meet in the same memory channels.
+  const int turn = EPI != kGradRows && nnt == 1 && g.parts == 1 && ksteps > 1 ? (int)((unsigned)mt * 5u % (unsigned)ksteps) : 0;
+  int cq = g.parts == 1 ? 0 : s0 / max(ksteps, 1), ck = (s0 - cq * ksteps + turn) * kStep, cs = 0, left = total;
   u32x4 ra, rb;
   A.aim(g.parts == 1 ? 0u : kPartA >> (2 * cq) & 3u, depth_a, ck);
   B.aim(g.parts == 1 ? 0u : kPartB >> (2 * cq) & 3u, depth_b, ck);
@@ -254,15 +254,13 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
     ck += kStep;
     A.move();
     B.move();
-    if (ck >= k_here) {
+    if (--left <= 0) {
+      A.left = B.left = 0;
+    } else if (ck >= k_here) {
       ck = 0;
-      ++cq;
-      if (g.parts > 1 && cq < 6) {
-        A.aim(kPartA >> (2 * cq) & 3u, depth_a, 0);
-        B.aim(kPartB >> (2 * cq) & 3u, depth_b, 0);
-      } else {
-        A.left = B.left = 0;
-      }
+      cq += g.parts > 1 ? 1 : 0;
+      A.aim(g.parts == 1 ? 0u : kPartA >> (2 * cq) & 3u, depth_a, 0);
+      B.aim(g.parts == 1 ? 0u : kPartB >> (2 * cq) & 3u, depth_b, 0);
     }
     ra = A.buffer();
     rb = B.buffer();
@@ -336,20 +334,6 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
     const int first_row = g.v0 + m0 + wm;
 #pragma unroll
     for (int j = 0; j < CB; ++j) {
-      const int n = n0 + wn + 32 * j + ln;
-      const uint32_t target = n < g.n ? row_of(g.targets, g.id_dtype, n, (uint32_t)g.V) : (uint32_t)g.V;
-      // The lane's place of the target's row: 16 i + r of those above, or none.
-      const uint32_t at_row = target - (uint32_t)first_row;
-      const uint32_t mine = target < (uint32_t)g.V && at_row < 32u * RB && (at_row >> 2 & 1u) == (uint32_t)lh
-                                ? (at_row >> 5) * 16u + (at_row >> 3 & 3u) * 4u + (at_row & 3u) : 0xffffu;
-      if (__any(mine != 0xffffu)) {
-        float z = 0.f;
-#pragma unroll
-        for (int i = 0; i < RB; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) z = mine == (uint32_t)(16 * i + r) ? acc[i][j][r] : z;
-        if (mine != 0xffffu) g.target_z[n] = z * g.scale;
-      }
       int rows = g.V - (first_row + 4 * lh);
       asm volatile("" : "+v"(rows));       // (compared anew: 64 masks kept for all j would not fit the scalar registers)
       const bool whole = first_row + 32 * RB <= g.V;
@@ -402,15 +386,18 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
         const int n = min(nb + ln, n_here - 1);
         const float lse = g.lse[n] * 1.44269504088896f, weight = g.weight[n], scale = g.scale * 1.44269504088896f;
         const int m_first = g.v0 + m0 + wm + 4 * lh;
-        int rows = g.V - m_first, hit = ((const int*)g.targets)[n] - m_first;
+        int rows = g.V - m_first, hit = g.targets[n] - m_first;
         asm volatile("" : "+v"(rows), "+v"(hit));
+        // (a target, or the table's end, among the wave's rows)
+        const bool special = __any((unsigned)hit < 32u * RB) || g.v0 + m0 + wm + 32 * RB > g.V;
 #pragma unroll
         for (int i = 0; i < RB; ++i)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int at = 32 * i + 8 * (r >> 2) + (r & 3);
             const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], scale, -lse));
-            acc[i][j][r] = at < rows ? (at == hit ? p - 1.f : p) * weight : 0.f;
+            acc[i][j][r] = p * weight;
+            if (special) acc[i][j][r] = at < rows ? (at == hit ? p - 1.f : p) * weight : 0.f;
           }
       }
 #pragma unroll
@@ -553,78 +540,136 @@ __global__ __launch_bounds__(kThreads) void kan_vocab_tokens_kernel(const TokenA
   }
 }
 
-// lse and loss of a token from the statistics of the table's tiles.
-__global__ __launch_bounds__(256) void kan_vocab_join_kernel(const float2* __restrict__ stats, int tiles, const float* __restrict__ target_z,
-                                                             const void* __restrict__ targets, int id_dtype, uint32_t V, int N, float* __restrict__ loss,
-                                                             float* __restrict__ lse) {
-  // 16 tokens a workgroup, 16 lanes share a token's tiles
-  __shared__ float2 sStat[16][16];
-  const int at = threadIdx.x & 15, share = threadIdx.x >> 4, n = blockIdx.x * 16 + at;
+// lse of a token from the statistics of the table's tiles, and its loss: the logit of its target is formed anew.
+struct JoinArgs {
+  const float2* stats;
+  const void *h, *table, *targets;
+  float *loss, *lse;
+  int tiles, N, D, id_dtype;
+  uint32_t V;
+  float scale;
+};
+template <class I, int TOKENS>
+__global__ __launch_bounds__(256) void kan_vocab_join_kernel(const JoinArgs a) {
+  // TOKENS a workgroup.  Statistics: TOKENS lanes side by side have a token each, the groups of them share the tiles; the
+  // target's logit: 256 / TOKENS lanes side by side have one token.
+  constexpr int G = 256 / TOKENS, U = TOKENS == 1 ? 4 : 16;
+  __shared__ float2 sStat[G][TOKENS];
+  __shared__ float sTarget[TOKENS][4];
+  const int at = threadIdx.x % TOKENS, share = threadIdx.x / TOKENS, n = blockIdx.x * TOKENS + at;
+  const int in = threadIdx.x % G, of = threadIdx.x / G, nt = blockIdx.x * TOKENS + of;
+  const uint32_t target = nt < a.N ? row_of(a.targets, a.id_dtype, nt, a.V) : a.V;
   float top = -FLT_MAX, sum = 0.f;
-  for (int t0 = share; t0 < tiles; t0 += 16 * 16) {
-    float2 s[16];
+  for (int t0 = share; t0 < a.tiles; t0 += U * G) {
+    float2 s[U];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s[k] = t0 + 16 * k < tiles && n < N ? stats[(long long)(t0 + 16 * k) * N + n] : make_float2(-FLT_MAX, 0.f);
+    for (int k = 0; k < U; ++k) s[k] = t0 + G * k < a.tiles && n < a.N ? a.stats[(long long)(t0 + G * k) * a.N + n] : make_float2(-FLT_MAX, 0.f);
     float m = top;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) m = fmaxf(m, s[k].x);
+    for (int k = 0; k < U; ++k) m = fmaxf(m, s[k].x);
     sum *= __builtin_amdgcn_exp2f(top - m);
 #pragma unroll
-    for (int k = 0; k < 16; ++k) sum += s[k].y * __builtin_amdgcn_exp2f(s[k].x - m);
+    for (int k = 0; k < U; ++k) sum += s[k].y * __builtin_amdgcn_exp2f(s[k].x - m);
     top = m;
   }
-  sStat[share][at] = make_float2(top, sum);
+  float dot = 0.f;
+  if (target < a.V) {
+    const I *const h = (const I*)a.h + (long long)nt * a.D, *const w = (const I*)a.table + (long long)target * a.D;
+#pragma unroll 4
+    for (int c = in * 8; c < a.D; c += G * 8) {
+      float x[8], y[8];
+      load_cols(h, c, a.D, x);
+      load_cols(w, c, a.D, y);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dot = fmaf(x[i], y[i], dot);
+    }
+  }
+#pragma unroll
+  for (int d = min(G, 64) / 2; d >= 1; d >>= 1) dot += __shfl_xor(dot, d);
+  if (in % 64 == 0) sTarget[of][in / 64] = dot;
+  if constexpr (TOKENS == 1) {       // a wave's share first
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+      const float t = __shfl_xor(top, d), u = __shfl_xor(sum, d), m = fmaxf(top, t);
+      sum = sum * __builtin_amdgcn_exp2f(top - m) + u * __builtin_amdgcn_exp2f(t - m);
+      top = m;
+    }
+  }
+  constexpr int R = TOKENS == 1 ? 4 : G;
+  if (TOKENS > 1 || share % 64 == 0) sStat[TOKENS == 1 ? share / 64 : share][at] = make_float2(top, sum);
   __syncthreads();
-  if (share == 0 && n < N) {
-    float m = top;
-    for (int k = 1; k < 16; ++k) m = fmaxf(m, sStat[k][at].x);
-    float s = 0.f;
-    for (int k = 0; k < 16; ++k) s += sStat[k][at].y * __builtin_amdgcn_exp2f(sStat[k][at].x - m);
+  if (share == 0 && n < a.N) {
+    float m = sStat[0][at].x, s = 0.f;
+#pragma unroll
+    for (int k = 1; k < R; ++k) m = fmaxf(m, sStat[k][at].x);
+#pragma unroll
+    for (int k = 0; k < R; ++k) s += sStat[k][at].y * __builtin_amdgcn_exp2f(sStat[k][at].x - m);
+    float z = 0.f;
+#pragma unroll
+    for (int k = 0; k < (G + 63) / 64; ++k) z += sTarget[at][k];
     const float l = 0.693147180559945f * (m + __builtin_amdgcn_logf(s));
-    lse[n] = l;
-    loss[n] = row_of(targets, id_dtype, n, V) < V ? l - target_z[n] : 0.f;
+    a.lse[n] = l;
+    a.loss[n] = row_of(a.targets, a.id_dtype, n, a.V) < a.V ? l - z * a.scale : 0.f;
   }
 }
 
-// dh from its slices: row i of them is token list[i]'s.
+// dh from its slices: row i of them is token list[i]'s.  SHARES groups of lanes add a share of the slices each.
+template <int SHARES>
 __global__ __launch_bounds__(kThreads) void kan_vocab_round_kernel(const float* __restrict__ src, int slices, long long slice, int N, int D, const Index x, int dtype,
                                                                    void* __restrict__ dst) {
-  const int C = (D + 7) / 8;
+  constexpr int kItems = kThreads / SHARES;
+  __shared__ float sSum[SHARES == 1 ? 1 : SHARES][kItems][9];
+  const int C = (D + 7) / 8, share = threadIdx.x / kItems, at = threadIdx.x % kItems;
   const long long items = (long long)min(*x.count, N) * C;
   const float f = *x.factor;
-  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < items; i += (long long)gridDim.x * kThreads) {
-    const long long row = i / C;
-    const int c = (int)(i - row * C) * 8;
+  for (long long i0 = (long long)blockIdx.x * kItems; i0 < items; i0 += (long long)gridDim.x * kItems) {
+    const long long i = i0 + at, row = min(i, items - 1) / C;
+    const int c = (int)(min(i, items - 1) - row * C) * 8;
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int k = 0; k < slices; ++k) {
+    for (int k = share; k < slices; k += SHARES) {
       float t[8];
       load_cols(src + k * slice + row * D, c, D, t);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += t[e];
     }
+    if constexpr (SHARES > 1) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= f;
-    store_any(dst, dtype, (long long)x.list[row] * D, c, D, v, false);
+      for (int e = 0; e < 8; ++e) sSum[share][at][e] = v[e];
+      __syncthreads();
+      if (share == 0)
+#pragma unroll
+        for (int k = 1; k < SHARES; ++k)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += sSum[k][at][e];
+    }
+    if (share == 0 && i < items) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= f;
+      store_any(dst, dtype, (long long)x.list[row] * D, c, D, v, false);
+    }
+    if constexpr (SHARES > 1) __syncthreads();
   }
 }
 
 // ---- which tiles, and how many shares of the contraction ---------------------------------------------------------------
 constexpr int kCus = 256;
-enum TileKind : int { k256x256, k256x128, k256x64, kTileKinds };
-constexpr int kTileM[] = {256, 256, 256}, kTileN[] = {256, 128, 64};
-// Clocks of a step of 32 and of a tile's beginning and end.
-constexpr long long kStepCost[] = {1024, 600, 420}, kTileCost[] = {12000, 8000, 6000};
+enum TileKind : int { k256x256, k256x128, k256x64, k128x64, kTileKinds };
+constexpr int kTileM[] = {256, 256, 256, 128}, kTileN[] = {256, 128, 64, 64};
+// Workgroups that share a CU (LDS); ns of a step of 32 and of a tile's beginning and end, with all of them on it (measured on
+// products of 8192 x 131072 x 2048 and 1111 x 50021 x 1000).
+constexpr long long kPerCu[] = {1, 1, 2, 3}, kStepNs[] = {850, 600, 660, 560}, kTileNs[] = {13500, 7200, 5800, 4300};
 
 long long tiles_of(int kind, long long m, long long n) { return ((m + kTileM[kind] - 1) / kTileM[kind]) * ((n + kTileN[kind] - 1) / kTileN[kind]); }
 
-// The tiles whose fullest CU is done first.
+// The tiles whose fullest CU is done first.  (A round that is not full runs with fewer workgroups a CU, which are faster then.)
 int pick_tiles(long long m, long long n, long long steps, int splits, long long* cost = nullptr) {
   int best = 0;
   long long least = -1;
   for (int kind = 0; kind < kTileKinds; ++kind) {
-    const long long rounds = (tiles_of(kind, m, n) * splits + kCus - 1) / kCus;
-    const long long c = rounds * (((steps + splits - 1) / splits) * kStepCost[kind] + kTileCost[kind]);
+    const long long each = ((steps + splits - 1) / splits) * kStepNs[kind] + kTileNs[kind], work = tiles_of(kind, m, n) * splits;
+    const long long full = work / (kCus * kPerCu[kind]), rest = work % (kCus * kPerCu[kind]);
+    const long long c = full * each + (rest ? each * ((rest + kCus - 1) / kCus + 1) / (kPerCu[kind] + 1) : 0);
     if (least < 0 || c < least) {
       least = c;
       best = kind;
@@ -638,10 +683,10 @@ int pick_tiles(long long m, long long n, long long steps, int splits, long long*
 int pick_splits(long long m, long long n, long long steps) {
   int best = 1;
   long long least = -1;
-  for (int s = 1; s <= 32 && steps / s >= 8; s *= 2) {
+  for (int s = 1; s <= 32 && steps / s >= 8; ++s) {
     long long c;
     pick_tiles(m, n, steps, s, &c);
-    if (s > 1) c += 4000 + m * n * 4 * s / 2000;
+    c += m * n * 8 * (s - 1) / 4000;
     if (least < 0 || c < least) {
       least = c;
       best = s;
@@ -650,14 +695,16 @@ int pick_splits(long long m, long long n, long long steps) {
   return best;
 }
 
+long long steps_of(long long k, int parts) { return (k + kStep - 1) / kStep * (parts == 1 ? 1 : 6); }
+
 template <class T, bool AK, bool BK, int EPI>
-hipError_t launch_product(const ProductArgs& g, hipStream_t s) {
-  const long long steps = (long long)((g.k + kStep - 1) / kStep) * (g.parts == 1 ? 1 : 6);
-  const int kind = pick_tiles(g.m, g.n, steps, g.splits);
+hipError_t launch_product(const ProductArgs& g, hipStream_t s, int kind = -1) {
+  if (kind < 0) kind = pick_tiles(g.m, g.n, steps_of(g.k, g.parts), g.splits);
   const dim3 grid((unsigned)(tiles_of(kind, g.m, g.n) * g.splits));
   if (kind == k256x256) hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 4, 4, 2, 2>), grid, dim3(kThreads), 0, s, g);
   else if (kind == k256x128) hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 4, 2, 2, 2>), grid, dim3(kThreads), 0, s, g);
-  else hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 2, 2, 4, 1>), grid, dim3(kThreads), 0, s, g);
+  else if (kind == k256x64) hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 2, 2, 4, 1>), grid, dim3(kThreads), 0, s, g);
+  else hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 2, 1, 2, 2>), grid, dim3(kThreads), 0, s, g);
   return hipGetLastError();
 }
 
@@ -667,7 +714,8 @@ struct Plan {
   long long width;            // columns of packed rows
   int piece, pieces;          // rows of the table that are dealt with at a time
   int slices;                 // of dh; 0: written at once
-  size_t h, table, stats, target_z, list, target, lse, weight, scalars, ds, dh, bytes;
+  int stat_kind;              // tiles of z (forward)
+  size_t h, table, stats, list, target, lse, weight, scalars, ds, dh, bytes;
 };
 
 Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
@@ -683,8 +731,7 @@ Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
   p.piece = (int)std::min(piece, (long long)INT32_MAX / kVocabStep * kVocabStep);
   p.pieces = (int)((V + (long long)p.piece - 1) / p.piece);
   if (backward) {
-    const long long steps = (std::min(p.piece, V) + kStep - 1) / kStep * (p.parts == 1 ? 1 : 6);
-    p.slices = pick_splits(D, N, steps);
+    p.slices = pick_splits(D, N, steps_of(std::min(p.piece, V), p.parts));
     if (p.slices == 1 && p.pieces == 1) p.slices = 0;
   }
   size_t at = 0;
@@ -696,8 +743,8 @@ Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
   p.h = take(backward || p.pack_table ? p.parts * N * p.width * 2 : 0);
   p.table = take(p.pack_table ? p.parts * (long long)p.piece * p.width * 2 : 0);
   if (!backward) {
-    p.stats = take((all / kTile) * N * 8);
-    p.target_z = take(N * 4);
+    p.stat_kind = pick_tiles(std::min(p.piece, V), N, steps_of(D, p.parts), 1);
+    p.stats = take(all / kTileM[p.stat_kind] * N * 8);
   } else {
     p.list = take(N * 4);
     p.target = take(N * 4);
@@ -767,10 +814,7 @@ kan_status run_vocab_loss(const VocabArgs& a, hipStream_t s) {
     g.splits = 1;
     g.V = a.V;
     g.scale = a.scale;
-    g.targets = a.targets;
-    g.id_dtype = a.id_dtype;
     g.stats = (float2*)(ws + p.stats);
-    g.target_z = (float*)(ws + p.target_z);
     kan_status st;
     g.b = {a.h, a.D, 0, (int)a.N, a.D};
     if (p.pack_table) {
@@ -781,13 +825,17 @@ kan_status run_vocab_loss(const VocabArgs& a, hipStream_t s) {
       g.v0 = v0;
       g.m = std::min(p.piece, a.V - v0);
       if ((st = table_rows(a, p, ws, v0, g.m, &g.a, s)) != KAN_OK) return st;
-      st = run_named("kan_vocab_loss", s, [&] { return launch_product<T, true, true, kStats>(g, s); });
+      st = run_named("kan_vocab_loss", s, [&] { return launch_product<T, true, true, kStats>(g, s, p.stat_kind); });
       if (st != KAN_OK) return st;
     }
     return run_named("kan_vocab_join", s, [&] {
-      hipLaunchKernelGGL(kan_vocab_join_kernel, dim3((unsigned)((a.N + 15) / 16)), dim3(256), 0, s, g.stats, (a.V + kTile - 1) / kTile, g.target_z, a.targets,
-                         a.id_dtype, (uint32_t)a.V, (int)a.N, a.loss, a.lse);
-      return hipGetLastError();
+      const int rows = kTileM[p.stat_kind];
+      const JoinArgs j = {g.stats, a.h, a.table, a.targets, a.loss, a.lse, (a.V + rows - 1) / rows, (int)a.N, a.D, a.id_dtype, (uint32_t)a.V, a.scale};
+      return with_float(a.dtype, [&](auto i) {
+        if (a.N <= 1024) hipLaunchKernelGGL((kan_vocab_join_kernel<decltype(i), 1>), dim3((unsigned)a.N), dim3(256), 0, s, j);
+        else hipLaunchKernelGGL((kan_vocab_join_kernel<decltype(i), 16>), dim3((unsigned)((a.N + 15) / 16)), dim3(256), 0, s, j);
+        return hipGetLastError();
+      });
     });
   });
 }
@@ -870,8 +918,13 @@ kan_status run_vocab_grad(const VocabArgs& a, hipStream_t s) {
     }
     if (!p.slices) return KAN_OK;
     return run_named("kan_vocab_round", s, [&] {
-      hipLaunchKernelGGL(kan_vocab_round_kernel, item_grid(a.N * ((a.D + 7) / 8)), dim3(kThreads), 0, s, (const float*)(ws + p.dh), p.slices, a.N * a.D, N, a.D, x,
-                         a.dtype, a.dh);
+      auto round = [&](auto shares) {
+        constexpr int S = decltype(shares)::value;
+        hipLaunchKernelGGL((kan_vocab_round_kernel<S>), item_grid(a.N * ((a.D + 7) / 8) * S), dim3(kThreads), 0, s, (const float*)(ws + p.dh), p.slices,
+                           a.N * a.D, N, a.D, x, a.dtype, a.dh);
+      };
+      if (p.slices >= 4 && a.N * a.D < (1 << 19)) round(std::integral_constant<int, 8>{});
+      else round(std::integral_constant<int, 1>{});
       return hipGetLastError();
     });
   });
