@@ -30,7 +30,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kStep = 32;               // products along the contraction per step
-constexpr int kSlots = 4;               // steps whose operands LDS holds
 constexpr int kVocabStep = 256;         // pieces of the table are multiples of it
 constexpr long long kPackBytes = 256ll << 20, kPieceBytes = 512ll << 20;
 
@@ -68,10 +67,9 @@ struct ProductArgs {
   const float *lse, *weight;
   void* ds;                  // [part][n][ds_stride]
   long long ds_stride, ds_part;
-  // kGradRows, kGradTable: out[n][m]; kGradRows: row n at place rows[n] of it
+  // kGradRows, kGradTable: out[n][m]
   void* out;
   long long out_stride, out_slice;
-  const int* rows;
   int out_dtype;
   int add;                   // add onto it
   const float* factor;       // null, or what the sums are multiplied with
@@ -199,16 +197,21 @@ struct Tile {
 
 // Workgroup of four waves: WM x WN of them, each RB x CB blocks of 32 x 32 results.
 //
-// A step is 32 of the contraction.  LDS holds four of them; the fragments of a step are read into registers while the step
-// before is multiplied, and the copies of the fourth next one are sent out, one or two between each two MFMAs.  One barrier
-// a step: behind it every wave's copies of step s + 1 have landed and nobody reads slot s % 4 any more.
-template <class T, bool AK, bool BK, int EPI, int RB, int CB, int WM, int WN>
-__global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const ProductArgs g) {
-  constexpr int BM = 32 * RB * WM, BN = 32 * CB * WN;
+// A step is 32 of the contraction.  LDS holds kSlots of them; the fragments of a step are read into registers while the step
+// before is multiplied, and the copies of the kSlots-th next one are sent out, one or two between each two MFMAs.  One barrier
+// a step: behind it every wave's copies of step s + 1 have landed and nobody reads slot s % kSlots any more.
+template <int RB_, int CB_, int WM_, int WN_, int SLOTS_>
+struct Shape {
+  static constexpr int RB = RB_, CB = CB_, WM = WM_, WN = WN_, kSlots = SLOTS_;
+  static constexpr int BM = 32 * RB * WM, BN = 32 * CB * WN, kLds = kSlots * (BM + BN) * kStep * 2;
+};
+
+template <class T, bool AK, bool BK, int EPI, class S>
+__device__ __forceinline__ void product(const ProductArgs& g, const unsigned block, unsigned char* const sRing) {
+  constexpr int RB = S::RB, CB = S::CB, WM = S::WM, WN = S::WN, kSlots = S::kSlots, BM = S::BM, BN = S::BN;
   typedef Tile<T, AK, BM> TA;
   typedef Tile<T, BK, BN> TB;
   constexpr int kSlot = TA::kBytes + TB::kBytes, kCopies = TA::kCopies + TB::kCopies;
-  __shared__ __attribute__((aligned(1024))) unsigned char sRing[kSlots * kSlot];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ln = lane & 31, lh = lane >> 5;
   const int wm = (wave % WM) * 32 * RB, wn = (wave / WM) * 32 * CB;
@@ -217,7 +220,7 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
   int mt, nt, split;
   const unsigned nmt = (unsigned)(g.m + BM - 1) / BM, nnt = (unsigned)(n_here + BN - 1) / BN, tiles = nmt * nnt, W = tiles * (unsigned)g.splits;
   {
-    const unsigned L = blockIdx.x, xcd = L & 7u, q = W >> 3, r = W & 7u;
+    const unsigned L = block, xcd = L & 7u, q = W >> 3, r = W & 7u;
     if (L >= W) return;
     const unsigned work = xcd * q + min(xcd, r) + (L >> 3), item = work % tiles;
     split = (int)(work / tiles);
@@ -245,12 +248,12 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
   B.aim(g.parts == 1 ? 0u : kPartB >> (2 * cq) & 3u, depth_b, ck);
   ra = A.buffer();
   rb = B.buffer();
-  auto copy = [&](int j) {
+  auto copy = [&](int j) __attribute__((always_inline)) {
     if (j < TA::kCopies) A.copy(ra, j, wave, lds0 + (uint32_t)(cs * kSlot), ck, depth_a);
     else B.copy(rb, j - TA::kCopies, wave, lds0 + (uint32_t)(cs * kSlot + TA::kBytes), ck, depth_b);
   };
-  auto next = [&] {
-    cs = (cs + 1) & (kSlots - 1);
+  auto next = [&]() __attribute__((always_inline)) {
+    cs = cs + 1 == kSlots ? 0 : cs + 1;
     ck += kStep;
     A.move();
     B.move();
@@ -283,7 +286,7 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
   };
   Frags f[2];
   constexpr int kReadsA = 2 * RB * TA::kReads, kReadsAll = kReadsA + 2 * CB * TB::kReads;
-  auto read = [&](const unsigned char* slot, int i, Frags& to) {
+  auto read = [&](const unsigned char* slot, int i, Frags& to) __attribute__((always_inline)) {
     if (i < kReadsA) {
       const int j = i % TA::kReads, b = i / TA::kReads % RB, h = i / TA::kReads / RB;
       A.fragment(slot, b, h, j, to.a[h][b]);
@@ -298,11 +301,13 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
 #pragma unroll
   for (int i = 0; i < kReadsAll; ++i) read(sRing, i, f[0]);
 
-  auto step = [&](auto P, int s) {
+  int rs = 0;
+  auto step = [&](auto P) __attribute__((always_inline)) {
     constexpr int p = decltype(P)::value, kMfmas = 2 * RB * CB, kSpread = kMfmas > 4 ? kMfmas - 2 : kMfmas;
     copies_done<(kSlots - 2) * kCopies>();
     __builtin_amdgcn_s_barrier();
-    const unsigned char* const slot = sRing + ((s + 1) & (kSlots - 1)) * kSlot;
+    rs = rs + 1 == kSlots ? 0 : rs + 1;
+    const unsigned char* const slot = sRing + rs * kSlot;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < kMfmas; ++i) {
@@ -319,10 +324,10 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
   };
   int s = 0;
   for (; s + 2 <= total; s += 2) {
-    step(std::integral_constant<int, 0>{}, s);
-    step(std::integral_constant<int, 1>{}, s + 1);
+    step(std::integral_constant<int, 0>{});
+    step(std::integral_constant<int, 1>{});
   }
-  if (s < total) step(std::integral_constant<int, 0>{}, s);
+  if (s < total) step(std::integral_constant<int, 0>{});
   copies_done<0>();
   __syncthreads();
 
@@ -376,6 +381,7 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
     // Blocks of 32 rows n go through LDS, each wave's through its own part, so that 4 RB lanes write the pieces of one row:
     // row r's four columns u at place u ^ r.
     constexpr int kUnits = 8 * RB, kGroup = 4 * RB;
+    static_assert(4 * 32 * kUnits * 16 <= S::kLds, "the blocks of four waves");
     float4* const mine = (float4*)sRing + wave * (32 * kUnits);
     const float factor = EPI != kGradS && g.factor ? *g.factor : 1.f;
 #pragma unroll
@@ -425,13 +431,26 @@ __global__ __launch_bounds__(kThreads, 1) void kan_vocab_product_kernel(const Pr
           if (m >= g.m) continue;
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[i] *= factor;
-          const long long row = EPI == kGradRows && g.rows ? g.rows[n] : n;
-          store_any(g.out, g.out_dtype, split * g.out_slice + row * g.out_stride, m, g.m, v, g.add);
+          store_any(g.out, g.out_dtype, split * g.out_slice + n * g.out_stride, m, g.m, v, g.add);
         }
       }
       __builtin_amdgcn_wave_barrier();
     }
   }
+}
+
+constexpr int waves_of(int lds) { return lds <= 81920 ? 2 : 1; }      // workgroups of four waves that a CU is to hold
+template <class T, bool AK, bool BK, int EPI, class S>
+__global__ __launch_bounds__(kThreads, waves_of(S::kLds)) void kan_vocab_product_kernel(const ProductArgs g) {
+  __shared__ __attribute__((aligned(1024))) unsigned char sRing[S::kLds];
+  product<T, AK, BK, EPI, S>(g, blockIdx.x, sRing);
+}
+// dh and dT of a piece in one launch, so that the tiles of one fill the CUs that the last round of the other leaves.
+template <class T, class S>
+__global__ __launch_bounds__(kThreads, waves_of(S::kLds)) void kan_vocab_grads_kernel(const ProductArgs rows, const ProductArgs table, unsigned row_blocks) {
+  __shared__ __attribute__((aligned(1024))) unsigned char sRing[S::kLds];
+  if (blockIdx.x < row_blocks) product<T, false, true, kGradRows, S>(rows, blockIdx.x, sRing);
+  else product<T, false, false, kGradTable, S>(table, blockIdx.x - row_blocks, sRing);
 }
 
 // Which tokens have a target that names a row: their numbers in order, from the back of the list those of the others; how
@@ -441,6 +460,10 @@ struct Index {
   int* count;
   float *mul, *factor;
 };
+// What the weights dloss are multiplied with, and what the sums are: fp16 dS has its largest weight at 2^14.
+__device__ __forceinline__ float scale_of(float scale, int half, float top) { return half ? (top > 0.f ? kHalfScale / top : 0.f) : scale; }
+__device__ __forceinline__ float factor_of(float scale, int half, float top) { return half ? scale * (top / kHalfScale) : 1.f; }
+
 __global__ __launch_bounds__(1024) void kan_vocab_index_kernel(const float* __restrict__ dloss, const void* __restrict__ targets, int id_dtype, uint32_t V, int N,
                                                                float scale, int half, const Index x) {
   __shared__ int sCount[16];
@@ -475,31 +498,46 @@ __global__ __launch_bounds__(1024) void kan_vocab_index_kernel(const float* __re
   if (threadIdx.x != 0) return;
   *x.count = before;
   for (int w = 0; w < 16; ++w) top = fmaxf(top, sMax[w]);
-  *x.mul = half ? (top > 0.f ? kHalfScale / top : 0.f) : scale;
-  *x.factor = half ? scale * (top / kHalfScale) : 1.f;
+  *x.mul = scale_of(scale, half, top);
+  *x.factor = factor_of(scale, half, top);
 }
 
 // Rows in the form the products take: 16-bit parts of `width` columns (zeros behind the last).
+struct PackArgs {
+  const void* src;
+  void* dst;
+  long long rows;
+};
 template <class I, class T, int PARTS>
-__global__ __launch_bounds__(kThreads) void kan_vocab_pack_kernel(const I* __restrict__ src, long long rows, int D, int width, long long part, T* __restrict__ dst) {
+__device__ __forceinline__ void pack_item(const I* row, int c, int D, T* dst, long long part) {
+  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (c < D) load_cols(row, c, D, v);
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p) {
+    store8(dst + p * part, v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] -= (float)(T)v[k];
+  }
+}
+template <class I, class T, int PARTS>
+__device__ __forceinline__ void pack_rows(const PackArgs& a, int D, int width, unsigned block, unsigned blocks) {
   const int C = width / 8;
-  const long long items = rows * C;
-  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < items; i += (long long)gridDim.x * kThreads) {
+  const long long items = a.rows * C;
+  for (long long i = (long long)block * kThreads + threadIdx.x; i < items; i += (long long)blocks * kThreads) {
     const long long row = i / C;
     const int c = (int)(i - row * C) * 8;
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (c < D) load_cols(src + row * D, c, D, v);
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) {
-      store8(dst + p * part + row * width + c, v);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] -= (float)(T)v[k];
-    }
+    pack_item<I, T, PARTS>((const I*)a.src + row * D, c, D, (T*)a.dst + row * width + c, a.rows * width);
   }
+}
+template <class I, class T, int PARTS>
+__global__ __launch_bounds__(kThreads) void kan_vocab_pack_kernel(const PackArgs a, const PackArgs b, unsigned blocks_a, int D, int width) {
+  if (blockIdx.x < blocks_a) pack_rows<I, T, PARTS>(a, D, width, blockIdx.x, blocks_a);
+  else pack_rows<I, T, PARTS>(b, D, width, blockIdx.x - blocks_a, gridDim.x - blocks_a);
 }
 
 // The same for the tokens that count, one behind the other, with their targets, lse and weights; zeros for the gradients of
-// the others.
+// the others.  Up to kOwnIndex tokens each workgroup counts the tokens in front of its own itself, beyond the index is there.
+constexpr int kOwnIndex = 4096, kTokensPerBlock = 4;
 struct TokenArgs {
   const void* h;
   const void* targets;
@@ -510,34 +548,85 @@ struct TokenArgs {
   Index x;
   int N, D, width, id_dtype;
   uint32_t V;
+  float scale;
+  int half, own_index;
+  unsigned blocks;
+  PackArgs table;            // and rows of the table by the workgroups behind
 };
 template <class I, class T, int PARTS>
-__global__ __launch_bounds__(kThreads) void kan_vocab_tokens_kernel(const TokenArgs a) {
-  const int C = a.width / 8, count = *a.x.count;
-  const long long items = (long long)a.N * C, part = (long long)a.N * a.width;
-  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < items; i += (long long)gridDim.x * kThreads) {
-    const long long at = i / C;
-    const int c = (int)(i - at * C) * 8;
-    const long long n = a.x.list[at];
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (at >= count) {
-      if (c < a.D) store_cols((I*)a.dh + n * a.D, c, a.D, v);
-      continue;
-    }
-    if (c < a.D) load_cols((const I*)a.h + n * a.D, c, a.D, v);
-    T* const dst = (T*)a.packed + at * a.width + c;
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) {
-      store8(dst + p * part, v);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] -= (float)(T)v[k];
-    }
-    if (c == 0) {
-      a.target[at] = (int)row_of(a.targets, a.id_dtype, n, a.V);
-      a.lse_out[at] = a.lse[n];
-      a.weight[at] = a.dloss[n] * *a.x.mul;
-    }
+__device__ __forceinline__ void pack_token(const TokenArgs& a, int n, int at, bool named, float mul, int c) {
+  if (!named) {
+    const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c < a.D) store_cols((I*)a.dh + (long long)n * a.D, c, a.D, zero);
+    return;
   }
+  pack_item<I, T, PARTS>((const I*)a.h + (long long)n * a.D, c, a.D, (T*)a.packed + (long long)at * a.width + c, (long long)a.N * a.width);
+  if (c == 0) {
+    a.target[at] = (int)row_of(a.targets, a.id_dtype, n, a.V);
+    a.lse_out[at] = a.lse[n];
+    a.weight[at] = a.dloss[n] * mul;
+  }
+}
+template <class I, class T, int PARTS>
+__global__ __launch_bounds__(kThreads) void kan_vocab_tokens_kernel(const TokenArgs a) {
+  if (blockIdx.x >= a.blocks) {
+    pack_rows<I, T, PARTS>(a.table, a.D, a.width, blockIdx.x - a.blocks, gridDim.x - a.blocks);
+    return;
+  }
+  if (!a.own_index) {
+    const int C = a.width / 8, count = *a.x.count;
+    const float mul = *a.x.mul;
+    const long long items = (long long)a.N * C;
+    for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < items; i += (long long)a.blocks * kThreads) {
+      const int at = (int)(i / C);
+      pack_token<I, T, PARTS>(a, a.x.list[at], at, at < count, mul, (int)(i - (long long)at * C) * 8);
+    }
+    return;
+  }
+  __shared__ int sFront[4], sAll[4];
+  __shared__ float sMax[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.x * kTokensPerBlock;
+  int front = 0, all = 0;
+  float top = 0.f;
+#pragma unroll 4
+  for (int n = threadIdx.x; n < a.N; n += kThreads)
+    if (row_of(a.targets, a.id_dtype, n, a.V) < a.V) {
+      ++all;
+      front += n < first ? 1 : 0;
+      if (a.half) top = fmaxf(top, fabsf(a.dloss[n]));
+    }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) {
+    front += __shfl_xor(front, d);
+    all += __shfl_xor(all, d);
+    top = fmaxf(top, __shfl_xor(top, d));
+  }
+  if (lane == 0) {
+    sFront[wave] = front;
+    sAll[wave] = all;
+    sMax[wave] = top;
+  }
+  __syncthreads();
+  front = sFront[0] + sFront[1] + sFront[2] + sFront[3];
+  all = sAll[0] + sAll[1] + sAll[2] + sAll[3];
+  top = fmaxf(fmaxf(sMax[0], sMax[1]), fmaxf(sMax[2], sMax[3]));
+  const float mul = scale_of(a.scale, a.half, top);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    *a.x.count = all;
+    *a.x.factor = factor_of(a.scale, a.half, top);
+  }
+  const int n = first + wave;           // a wave has a token
+  if (n >= a.N) return;
+  int at = front;
+  bool named = false;
+#pragma unroll
+  for (int k = 0; k < kTokensPerBlock; ++k) {
+    const bool t = first + k < a.N && row_of(a.targets, a.id_dtype, min(first + k, a.N - 1), a.V) < a.V;
+    at += k < wave && t ? 1 : 0;
+    named = k == wave ? t : named;
+  }
+  if (lane == 0 && named) a.x.list[at] = n;
+  for (int c = lane * 8; c < a.width; c += 512) pack_token<I, T, PARTS>(a, n, at, named, mul, c);
 }
 
 // lse of a token from the statistics of the table's tiles, and its loss: the logit of its target is formed anew.
@@ -656,56 +745,82 @@ __global__ __launch_bounds__(kThreads) void kan_vocab_round_kernel(const float* 
 constexpr int kCus = 256;
 enum TileKind : int { k256x256, k256x128, k256x64, k128x64, kTileKinds };
 constexpr int kTileM[] = {256, 256, 256, 128}, kTileN[] = {256, 128, 64, 64};
-// Workgroups that share a CU (LDS); ns of a step of 32 and of a tile's beginning and end, with all of them on it (measured on
-// products of 8192 x 131072 x 2048 and 1111 x 50021 x 1000).
-constexpr long long kPerCu[] = {1, 1, 2, 3}, kStepNs[] = {850, 600, 660, 560}, kTileNs[] = {13500, 7200, 5800, 4300};
+// Workgroups that share a CU, ns of a step of 32 with all of them on it, and ns of a tile's beginning and end: with the
+// statistics of z, and with rows that leave through LDS (measured on products of 8192 x 131072 x 2048, 1111 x 50021 x 1000 and
+// 16 x 65536 x 2048).
+constexpr long long kPerCu[] = {1, 2, 2, 3}, kStepNs[] = {850, 1040, 660, 560};
+constexpr long long kStatNs[] = {5000, 4000, 4500, 4000}, kRowsNs[] = {13000, 8000, 5800, 4300};
 
 long long tiles_of(int kind, long long m, long long n) { return ((m + kTileM[kind] - 1) / kTileM[kind]) * ((n + kTileN[kind] - 1) / kTileN[kind]); }
+long long steps_of(long long k, int parts) { return (k + kStep - 1) / kStep * (parts == 1 ? 1 : 6); }
+long long tile_ns(int kind, long long steps, bool stats) { return steps * kStepNs[kind] + (stats ? kStatNs : kRowsNs)[kind]; }
 
-// The tiles whose fullest CU is done first.  (A round that is not full runs with fewer workgroups a CU, which are faster then.)
-int pick_tiles(long long m, long long n, long long steps, int splits, long long* cost = nullptr) {
+// ns until the fullest CU is done.  (A round that is not full has fewer workgroups a CU, which are faster then.)
+long long rounds_ns(int kind, long long tiles, long long each) {
+  const long long full = tiles / (kCus * kPerCu[kind]), rest = tiles % (kCus * kPerCu[kind]);
+  return full * each + (rest ? each * ((rest + kCus - 1) / kCus + 1) / (kPerCu[kind] + 1) : 0);
+}
+
+// The tiles that are done first.
+int pick_tiles(long long m, long long n, long long steps, bool stats) {
   int best = 0;
   long long least = -1;
   for (int kind = 0; kind < kTileKinds; ++kind) {
-    const long long each = ((steps + splits - 1) / splits) * kStepNs[kind] + kTileNs[kind], work = tiles_of(kind, m, n) * splits;
-    const long long full = work / (kCus * kPerCu[kind]), rest = work % (kCus * kPerCu[kind]);
-    const long long c = full * each + (rest ? each * ((rest + kCus - 1) / kCus + 1) / (kPerCu[kind] + 1) : 0);
+    const long long c = rounds_ns(kind, tiles_of(kind, m, n), tile_ns(kind, steps, stats));
     if (least < 0 || c < least) {
       least = c;
       best = kind;
     }
   }
-  if (cost) *cost = least;
   return best;
 }
 
-// Shares of a long contraction that few tiles have: each adds a slice of n x m sums that is written and read once.
-int pick_splits(long long m, long long n, long long steps) {
-  int best = 1;
+// dh and dT of a piece of V rows: tiles of both, and the shares in which dh's long contraction is done where it has few tiles:
+// each adds a slice of N x D sums that is written and read once.
+void pick_grads(long long N, long long V, long long D, int parts, int* kind, int* slices) {
   long long least = -1;
-  for (int s = 1; s <= 32 && steps / s >= 8; ++s) {
-    long long c;
-    pick_tiles(m, n, steps, s, &c);
-    c += m * n * 8 * (s - 1) / 4000;
-    if (least < 0 || c < least) {
-      least = c;
-      best = s;
+  const long long steps = steps_of(V, parts);
+  for (int k = 0; k < kTileKinds; ++k)
+    for (int s = 1; s <= 32 && (s == 1 || steps / s >= 8); ++s) {
+      const long long rows = tile_ns(k, (steps + s - 1) / s, false), table = tile_ns(k, steps_of(N, parts), false);
+      const long long n1 = tiles_of(k, D, N) * s, n2 = tiles_of(k, D, V), slots = kCus * kPerCu[k];
+      // the CUs' work in all, and the end of a round of it; or what is longest, if there is no more than a round
+      long long c = n1 + n2 > slots ? (n1 * rows + n2 * table) / slots + std::max(rows, table) / 2 : std::max(rows, table);
+      c += N * D * 8 * (s - 1) / 4000;
+      if (least < 0 || c < least) {
+        least = c;
+        *kind = k;
+        *slices = s;
+      }
     }
-  }
-  return best;
 }
 
-long long steps_of(long long k, int parts) { return (k + kStep - 1) / kStep * (parts == 1 ? 1 : 6); }
+// f(S{}) for the shape of a kind.
+template <class F>
+hipError_t with_tiles(int kind, F&& f) {
+  if (kind == k256x256) return f(Shape<4, 4, 2, 2, 4>{});
+  if (kind == k256x128) return f(Shape<4, 2, 2, 2, 3>{});
+  if (kind == k256x64) return f(Shape<2, 2, 4, 1, 4>{});
+  return f(Shape<2, 1, 2, 2, 4>{});
+}
 
-template <class T, bool AK, bool BK, int EPI>
-hipError_t launch_product(const ProductArgs& g, hipStream_t s, int kind = -1) {
-  if (kind < 0) kind = pick_tiles(g.m, g.n, steps_of(g.k, g.parts), g.splits);
-  const dim3 grid((unsigned)(tiles_of(kind, g.m, g.n) * g.splits));
-  if (kind == k256x256) hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 4, 4, 2, 2>), grid, dim3(kThreads), 0, s, g);
-  else if (kind == k256x128) hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 4, 2, 2, 2>), grid, dim3(kThreads), 0, s, g);
-  else if (kind == k256x64) hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 2, 2, 4, 1>), grid, dim3(kThreads), 0, s, g);
-  else hipLaunchKernelGGL((kan_vocab_product_kernel<T, AK, BK, EPI, 2, 1, 2, 2>), grid, dim3(kThreads), 0, s, g);
-  return hipGetLastError();
+template <class T, int EPI>
+hipError_t launch_product(const ProductArgs& g, int kind, hipStream_t s) {
+  return with_tiles(kind, [&](auto shape) {
+    hipLaunchKernelGGL((kan_vocab_product_kernel<T, true, true, EPI, decltype(shape)>), dim3((unsigned)tiles_of(kind, g.m, g.n)), dim3(kThreads), 0, s, g);
+    return hipGetLastError();
+  });
+}
+
+template <class T>
+hipError_t launch_grads(const ProductArgs& rows, const ProductArgs& table, int kind, hipStream_t s) {
+  // (a multiple of eight, so that the second product's workgroups find their XCDs as the first's do)
+  const unsigned row_blocks = (unsigned)((tiles_of(kind, rows.m, rows.n) * rows.splits + 7) / 8 * 8);
+  return with_tiles(kind, [&](auto shape) {
+    hipLaunchKernelGGL((kan_vocab_grads_kernel<T, decltype(shape)>), dim3(row_blocks + (unsigned)tiles_of(kind, table.m, table.n)), dim3(kThreads), 0, s, rows,
+                       table, row_blocks);
+    return hipGetLastError();
+  });
 }
 
 struct Plan {
@@ -713,8 +828,8 @@ struct Plan {
   bool pack_table;            // the table's rows go through the workspace
   long long width;            // columns of packed rows
   int piece, pieces;          // rows of the table that are dealt with at a time
-  int slices;                 // of dh; 0: written at once
-  int stat_kind;              // tiles of z (forward)
+  int slices;                 // of dh
+  int z_kind, grad_kind;      // tiles of z, of dh and dT
   size_t h, table, stats, list, target, lse, weight, scalars, ds, dh, bytes;
 };
 
@@ -730,10 +845,8 @@ Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
   if (backward) limit(kPieceBytes, p.parts * N * 2);
   p.piece = (int)std::min(piece, (long long)INT32_MAX / kVocabStep * kVocabStep);
   p.pieces = (int)((V + (long long)p.piece - 1) / p.piece);
-  if (backward) {
-    p.slices = pick_splits(D, N, steps_of(std::min(p.piece, V), p.parts));
-    if (p.slices == 1 && p.pieces == 1) p.slices = 0;
-  }
+  p.z_kind = pick_tiles(std::min(p.piece, V), N, steps_of(D, p.parts), !backward);
+  if (backward) pick_grads(N, std::min(p.piece, V), D, p.parts, &p.grad_kind, &p.slices);
   size_t at = 0;
   auto take = [&](long long bytes) {
     const size_t was = at;
@@ -743,8 +856,7 @@ Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
   p.h = take(backward || p.pack_table ? p.parts * N * p.width * 2 : 0);
   p.table = take(p.pack_table ? p.parts * (long long)p.piece * p.width * 2 : 0);
   if (!backward) {
-    p.stat_kind = pick_tiles(std::min(p.piece, V), N, steps_of(D, p.parts), 1);
-    p.stats = take(all / kTileM[p.stat_kind] * N * 8);
+    p.stats = take(all / kTileM[p.z_kind] * N * 8);
   } else {
     p.list = take(N * 4);
     p.target = take(N * 4);
@@ -766,15 +878,15 @@ hipError_t with_parts(int dtype, F&& f) {
   return f(bf16{}, bf16{}, std::integral_constant<int, 1>{});
 }
 
-dim3 item_grid(long long items) { return dim3((unsigned)std::min((items + kThreads - 1) / kThreads, 1ll << 15)); }
+unsigned item_blocks(long long items) { return (unsigned)std::min((items + kThreads - 1) / kThreads, 1ll << 15); }
 
-kan_status pack(const void* src, long long rows, int D, long long width, int dtype, void* dst, hipStream_t s) {
+// Rows of a, and of b (none: no rows), in the form the products take.
+kan_status pack(const PackArgs& a, const PackArgs& b, int D, long long width, int dtype, hipStream_t s) {
   return run_named("kan_vocab_pack", s, [&] {
     return with_parts(dtype, [&](auto i, auto t, auto parts) {
-      typedef decltype(i) I;
-      typedef decltype(t) T;
-      hipLaunchKernelGGL((kan_vocab_pack_kernel<I, T, decltype(parts)::value>), item_grid(rows * (width / 8)), dim3(kThreads), 0, s, (const I*)src, rows, D,
-                         (int)width, rows * width, (T*)dst);
+      const unsigned first = item_blocks(a.rows * (width / 8)), second = item_blocks(b.rows * (width / 8));
+      hipLaunchKernelGGL((kan_vocab_pack_kernel<decltype(i), decltype(t), decltype(parts)::value>), dim3(first + second), dim3(kThreads), 0, s, a, b, first, D,
+                         (int)width);
       return hipGetLastError();
     });
   });
@@ -787,15 +899,13 @@ kan_status with_operand(int dtype, F&& f) {
   return f(bf16{});
 }
 
-// The rows of the table from v0 on as an operand whose k is the width.
-kan_status table_rows(const VocabArgs& a, const Plan& p, unsigned char* ws, int v0, int rows, Operand* out, hipStream_t s) {
+// The rows of the table from v0 on as an operand whose k is the width, and what has to be packed for it.
+Operand table_rows(const VocabArgs& a, const Plan& p, unsigned char* ws, int v0, int rows, PackArgs* job) {
   const char* const src = (const char*)a.table + (long long)v0 * a.D * float_bytes(a.dtype);
-  if (!p.pack_table) {
-    *out = {src, a.D, 0, rows, a.D};
-    return KAN_OK;
-  }
-  *out = {ws + p.table, p.width, rows * p.width, rows, (int)p.width};
-  return pack(src, rows, a.D, p.width, a.dtype, ws + p.table, s);
+  *job = {};
+  if (!p.pack_table) return {src, a.D, 0, rows, a.D};
+  *job = {src, ws + p.table, rows};
+  return {ws + p.table, p.width, rows * p.width, rows, (int)p.width};
 }
 
 }  // namespace
@@ -816,20 +926,21 @@ kan_status run_vocab_loss(const VocabArgs& a, hipStream_t s) {
     g.scale = a.scale;
     g.stats = (float2*)(ws + p.stats);
     kan_status st;
-    g.b = {a.h, a.D, 0, (int)a.N, a.D};
-    if (p.pack_table) {
-      if ((st = pack(a.h, a.N, a.D, p.width, a.dtype, ws + p.h, s)) != KAN_OK) return st;
-      g.b = {ws + p.h, p.width, a.N * p.width, (int)a.N, (int)p.width};
-    }
+    g.b = p.pack_table ? Operand{ws + p.h, p.width, a.N * p.width, (int)a.N, (int)p.width} : Operand{a.h, a.D, 0, (int)a.N, a.D};
     for (int v0 = 0, i = 0; i < p.pieces; ++i, v0 += p.piece) {
+      PackArgs job;
       g.v0 = v0;
       g.m = std::min(p.piece, a.V - v0);
-      if ((st = table_rows(a, p, ws, v0, g.m, &g.a, s)) != KAN_OK) return st;
-      st = run_named("kan_vocab_loss", s, [&] { return launch_product<T, true, true, kStats>(g, s, p.stat_kind); });
+      g.a = table_rows(a, p, ws, v0, g.m, &job);
+      if (p.pack_table) {
+        const PackArgs rows = {a.h, ws + p.h, i == 0 ? a.N : 0};
+        if ((st = pack(job, rows, a.D, p.width, a.dtype, s)) != KAN_OK) return st;
+      }
+      st = run_named("kan_vocab_loss", s, [&] { return launch_product<T, kStats>(g, p.z_kind, s); });
       if (st != KAN_OK) return st;
     }
     return run_named("kan_vocab_join", s, [&] {
-      const int rows = kTileM[p.stat_kind];
+      const int rows = kTileM[p.z_kind];
       const JoinArgs j = {g.stats, a.h, a.table, a.targets, a.loss, a.lse, (a.V + rows - 1) / rows, (int)a.N, a.D, a.id_dtype, (uint32_t)a.V, a.scale};
       return with_float(a.dtype, [&](auto i) {
         if (a.N <= 1024) hipLaunchKernelGGL((kan_vocab_join_kernel<decltype(i), 1>), dim3((unsigned)a.N), dim3(256), 0, s, j);
@@ -845,28 +956,39 @@ kan_status run_vocab_grad(const VocabArgs& a, hipStream_t s) {
   unsigned char* const ws = (unsigned char*)a.ws;
   const int N = (int)a.N;
   const Index x = {(int*)(ws + p.list), (int*)(ws + p.scalars), (float*)(ws + p.scalars) + 1, (float*)(ws + p.scalars) + 2};
-  kan_status st = run_named("kan_vocab_index", s, [&] {
-    hipLaunchKernelGGL(kan_vocab_index_kernel, dim3(1), dim3(1024), 0, s, a.dloss, a.targets, a.id_dtype, (uint32_t)a.V, N, a.scale, a.dtype == KAN_F16, x);
-    return hipGetLastError();
-  });
-  if (st != KAN_OK) return st;
-  const TokenArgs ta = {a.h, a.targets, a.lse, a.dloss, ws + p.h, a.dh, (int*)(ws + p.target), (float*)(ws + p.lse), (float*)(ws + p.weight), x, N, a.D,
-                        (int)p.width, a.id_dtype, (uint32_t)a.V};
-  st = run_named("kan_vocab_tokens", s, [&] {
-    return with_parts(a.dtype, [&](auto i, auto t, auto parts) {
-      hipLaunchKernelGGL((kan_vocab_tokens_kernel<decltype(i), decltype(t), decltype(parts)::value>), item_grid(N * (p.width / 8)), dim3(kThreads), 0, s, ta);
+  const bool own_index = N <= kOwnIndex;
+  kan_status st = KAN_OK;
+  if (!own_index) {
+    st = run_named("kan_vocab_index", s, [&] {
+      hipLaunchKernelGGL(kan_vocab_index_kernel, dim3(1), dim3(1024), 0, s, a.dloss, a.targets, a.id_dtype, (uint32_t)a.V, N, a.scale, a.dtype == KAN_F16, x);
       return hipGetLastError();
     });
-  });
-  if (st != KAN_OK) return st;
+    if (st != KAN_OK) return st;
+  }
+  TokenArgs ta = {a.h, a.targets, a.lse, a.dloss, ws + p.h, a.dh, (int*)(ws + p.target), (float*)(ws + p.lse), (float*)(ws + p.weight), x, N, a.D, (int)p.width,
+                  a.id_dtype, (uint32_t)a.V, a.scale, a.dtype == KAN_F16, own_index, 0, {}};
+  ta.blocks = own_index ? (unsigned)(N + kTokensPerBlock - 1) / kTokensPerBlock : item_blocks(N * (p.width / 8));
   return with_operand(a.dtype, [&](auto t) -> kan_status {
     typedef decltype(t) T;
     const Operand h = {ws + p.h, p.width, a.N * p.width, N, (int)p.width};
     for (int v0 = 0, i = 0; i < p.pieces; ++i, v0 += p.piece) {
       const int rows = std::min(p.piece, a.V - v0);
       const long long ds_part = a.N * (long long)p.piece;
-      Operand table;
-      if ((st = table_rows(a, p, ws, v0, rows, &table, s)) != KAN_OK) return st;
+      PackArgs job;
+      const Operand table = table_rows(a, p, ws, v0, rows, &job);
+      if (i == 0) {
+        ta.table = job;
+        st = run_named("kan_vocab_tokens", s, [&] {
+          return with_parts(a.dtype, [&](auto in, auto out, auto parts) {
+            hipLaunchKernelGGL((kan_vocab_tokens_kernel<decltype(in), decltype(out), decltype(parts)::value>),
+                               dim3(ta.blocks + item_blocks(job.rows * (p.width / 8))), dim3(kThreads), 0, s, ta);
+            return hipGetLastError();
+          });
+        });
+      } else if (p.pack_table) {
+        st = pack(job, PackArgs{}, a.D, p.width, a.dtype, s);
+      }
+      if (st != KAN_OK) return st;
       ProductArgs g = {};
       g.count = x.count;
       g.parts = p.parts;
@@ -885,42 +1007,38 @@ kan_status run_vocab_grad(const VocabArgs& a, hipStream_t s) {
       g.k = a.D;
       g.a = table;
       g.b = h;
-      st = run_named("kan_vocab_ds", s, [&] { return launch_product<T, true, true, kGradS>(g, s); });
+      st = run_named("kan_vocab_ds", s, [&] { return launch_product<T, kGradS>(g, p.z_kind, s); });
       if (st != KAN_OK) return st;
       // dh (+)= dS T: k = rows of the piece
-      g.m = a.D;
-      g.k = rows;
-      g.splits = std::max(1, p.slices);
-      g.a = {table.p, table.stride, table.part, a.D, rows};
-      g.b = {ws + p.ds, p.piece, ds_part, N, (rows + 7) / 8 * 8};      // (zeros behind the last row)
-      g.out = p.slices ? (void*)(ws + p.dh) : a.dh;
-      g.out_stride = a.D;
-      g.out_slice = a.N * a.D;
-      g.out_dtype = p.slices ? KAN_F32 : a.dtype;
-      g.rows = p.slices ? nullptr : x.list;
-      g.add = i > 0;
-      g.factor = p.slices ? nullptr : x.factor;
-      st = run_named("kan_vocab_dh", s, [&] { return launch_product<T, false, true, kGradRows>(g, s); });
-      if (st != KAN_OK) return st;
+      ProductArgs r = g;
+      r.m = a.D;
+      r.k = rows;
+      r.splits = p.slices;
+      r.a = {table.p, table.stride, table.part, a.D, rows};
+      r.b = {ws + p.ds, p.piece, ds_part, N, (rows + 7) / 8 * 8};      // (zeros behind the last row)
+      r.out = ws + p.dh;
+      r.out_stride = a.D;
+      r.out_slice = a.N * a.D;
+      r.out_dtype = KAN_F32;
+      r.add = i > 0;
       // dT (+)= dS^t h: k = tokens
+      g.m = a.D;
       g.n = rows;
       g.k = N;
-      g.splits = 1;
       g.a = {h.p, h.stride, h.part, a.D, N};
       g.b = {ws + p.ds, p.piece, ds_part, rows, N};
       g.out = (char*)a.dtable + (long long)v0 * a.D * float_bytes(a.dtype);
+      g.out_stride = a.D;
       g.out_dtype = a.dtype;
-      g.rows = nullptr;
       g.add = a.accumulate;
       g.factor = x.factor;
-      st = run_named("kan_vocab_dtable", s, [&] { return launch_product<T, false, false, kGradTable>(g, s); });
+      st = run_named("kan_vocab_grads", s, [&] { return launch_grads<T>(r, g, p.grad_kind, s); });
       if (st != KAN_OK) return st;
     }
-    if (!p.slices) return KAN_OK;
     return run_named("kan_vocab_round", s, [&] {
       auto round = [&](auto shares) {
         constexpr int S = decltype(shares)::value;
-        hipLaunchKernelGGL((kan_vocab_round_kernel<S>), item_grid(a.N * ((a.D + 7) / 8) * S), dim3(kThreads), 0, s, (const float*)(ws + p.dh), p.slices,
+        hipLaunchKernelGGL((kan_vocab_round_kernel<S>), dim3(item_blocks(a.N * ((a.D + 7) / 8) * S)), dim3(kThreads), 0, s, (const float*)(ws + p.dh), p.slices,
                            a.N * a.D, N, a.D, x, a.dtype, a.dh);
       };
       if (p.slices >= 4 && a.N * a.D < (1 << 19)) round(std::integral_constant<int, 8>{});
