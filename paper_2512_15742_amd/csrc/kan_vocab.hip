@@ -784,8 +784,8 @@ void pick_grads(long long N, long long V, long long D, int parts, int* kind, int
     for (int s = 1; s <= 32 && (s == 1 || steps / s >= 8); ++s) {
       const long long rows = tile_ns(k, (steps + s - 1) / s, false), table = tile_ns(k, steps_of(N, parts), false);
       const long long n1 = tiles_of(k, D, N) * s, n2 = tiles_of(k, D, V), slots = kCus * kPerCu[k];
-      // the CUs' work in all, and the end of a round of it; or what is longest, if there is no more than a round
-      long long c = n1 + n2 > slots ? (n1 * rows + n2 * table) / slots + std::max(rows, table) / 2 : std::max(rows, table);
+      // dh's rounds, or the CUs' work in all and the end of the last tiles, which are dT's
+      long long c = std::max((n1 + slots - 1) / slots * rows, n1 + n2 > slots ? (n1 * rows + n2 * table) / slots + table / 2 : std::max(rows, table));
       c += N * D * 8 * (s - 1) / 4000;
       if (least < 0 || c < least) {
         least = c;
