@@ -31,7 +31,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;
 constexpr int kStep = 32;               // products along the contraction per step
 constexpr int kVocabStep = 256;         // pieces of the table are multiples of it
-constexpr long long kPackBytes = 256ll << 20, kPieceBytes = 512ll << 20;
+constexpr long long kPackBytes = 256ll << 20, kPieceBytes = 256ll << 20;
 
 constexpr float kHalfScale = 16384.f;   // of fp16 dS
 
