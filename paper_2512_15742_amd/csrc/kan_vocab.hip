@@ -160,18 +160,22 @@ struct Tile {
   }
   // The buffer of the next copies: aimed at some k of a part, then moved on a step at a time.
   uint64_t at;
-  long long left;                  // bytes from there to the end of the operand
+  uint32_t bytes;                  // k contiguous: from there to the end of the last row; strided: of one k
+  int deep;                        // k that are left
   __device__ __forceinline__ void aim(uint32_t p, int depth, int k0) {
-    const long long from = (long long)(k0 / kStep) * step;
-    at = (uint64_t)(uintptr_t)base + (uint64_t)((long long)p * part + from);
-    left = (K ? limit : (long long)depth * limit - (long long)chunk) - from;
+    at = (uint64_t)(uintptr_t)base + (uint64_t)((long long)p * part + (long long)(k0 / kStep) * step);
+    bytes = K ? (uint32_t)limit - (uint32_t)k0 * 2u : (uint32_t)limit;
+    deep = depth - k0;
   }
   __device__ __forceinline__ void move() {
-    at += (uint64_t)step;
-    left -= step;
+    at += (uint32_t)step;
+    if (K) bytes -= kStep * 2u;
+    deep -= kStep;
   }
   __device__ __forceinline__ u32x4 buffer() const {
-    u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32), (uint32_t)max(min(left, 0x7fffff00ll), 0ll), 0x00020000u};
+    // (a strided step's last row ends where the tile's columns begin behind it: fewer bytes by r0)
+    const uint32_t n = K ? bytes : (uint32_t)min(deep, kStep) * bytes - chunk;
+    u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32), deep > 0 ? n : 0u, 0x00020000u};
     return r;
   }
   __device__ __forceinline__ void copy(const u32x4& r, int j, int wave, uint32_t lds, int k0, int depth) const {
@@ -258,7 +262,7 @@ __device__ __forceinline__ void product(const ProductArgs& g, const unsigned blo
     A.move();
     B.move();
     if (--left <= 0) {
-      A.left = B.left = 0;
+      A.deep = B.deep = 0;
     } else if (ck >= k_here) {
       ck = 0;
       cq += g.parts > 1 ? 1 : 0;
@@ -842,7 +846,13 @@ Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
   long long piece = all;
   auto limit = [&](long long budget, long long row_bytes) { piece = std::min(piece, std::max(1ll, budget / (row_bytes * kVocabStep)) * kVocabStep); };
   if (p.pack_table) limit(kPackBytes, p.parts * p.width * 2);
-  if (backward) limit(kPieceBytes, p.parts * N * 2);
+  // (tiles of 128 x 64: fewer than 2^23 of a launch's)
+  limit(1ll << 36, N);
+  if (backward) {
+    limit(kPieceBytes, p.parts * N * 2);
+    limit(1ll << 36, D);
+    limit(1ll << 25, 1);           // (32 rows of dS: 32-bit offsets)
+  }
   p.piece = (int)std::min(piece, (long long)INT32_MAX / kVocabStep * kVocabStep);
   p.pieces = (int)((V + (long long)p.piece - 1) / p.piece);
   p.z_kind = pick_tiles(std::min(p.piece, V), N, steps_of(D, p.parts), !backward);
