@@ -25,16 +25,44 @@ constexpr int kMaxGroups = 512;         // groups of waves of a backward launch,
 constexpr int kMaxBlocks = 1 << 20;     // workgroups of a forward launch: they take rows in turn
 constexpr int kReduceThreads = 1024;    // 16 columns, 64 shares of the groups
 
+// Rows whose width is no multiple of eight: a lane's eight columns begin where row n's place in the array is one, so that all
+// its accesses are aligned; those in front of the row (c < 0) and behind it are left out.
+// WHOLE: widths that are multiples of eight, no lane has a part of eight columns.
+template <bool WHOLE, int COLS>      // columns that the lanes have
+__device__ __forceinline__ int first_shift(long long n, int D) { return !WHOLE && D + 7 <= COLS ? (int)((n * D) & 7) : 0; }
+template <bool WHOLE>
+__device__ __forceinline__ bool within(int c, int D) { return WHOLE || (c >= 0 && c + 8 <= D); }
+template <bool WHOLE, class T>
+__device__ __forceinline__ void load_part(const T* row, int c, int D, float (&out)[8]) {
+  if (within<WHOLE>(c, D)) {
+    load8(row + c, out);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] = c + i >= 0 && c + i < D ? (float)row[c + i] : 0.f;
+  }
+}
+template <bool WHOLE, class T>
+__device__ __forceinline__ void store_part(T* row, int c, int D, const float (&in)[8]) {
+  if (within<WHOLE>(c, D)) {
+    store8(row + c, in);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i >= 0 && c + i < D) row[c + i] = (T)in[i];
+  }
+}
+
+template <bool WHOLE>
 __device__ __forceinline__ void load_weight(const void* w, int dtype, int c, int D, float (&out)[8]) {
   if (!w) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) out[i] = 1.f;
   } else if (dtype == KAN_F32) {
-    load_cols((const float*)w, c, D, out);
+    load_part<WHOLE>((const float*)w, c, D, out);
   } else if (dtype == KAN_F16) {
-    load_cols((const f16*)w, c, D, out);
+    load_part<WHOLE>((const f16*)w, c, D, out);
   } else {
-    load_cols((const bf16*)w, c, D, out);
+    load_part<WHOLE>((const bf16*)w, c, D, out);
   }
 }
 
@@ -65,7 +93,7 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float (*scratch)[K]) {
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 
 // W waves a row, W == 1: four rows a workgroup.
-template <class S, class B, int W, int P>
+template <class S, class B, int W, int P, bool WHOLE>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_kernel(const NormArgs a) {
   __shared__ float sSum[2][W][1];
   const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x;
@@ -74,17 +102,18 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_kernel(const N
   const long long rows = (long long)gridDim.x * (W == 1 ? 4 : 1);
   for (long long n = W == 1 ? (long long)blockIdx.x * 4 + (threadIdx.x >> 6) : (long long)blockIdx.x; n < a.N; n += rows) {
     float x[P][8], v[P][8], g[P][8], w[P][8];
+    const int shift = first_shift<WHOLE, 512 * W * P>(n, D);
   #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const int c = (p * 64 * W + t) * 8;
+      const int c = (p * 64 * W + t) * 8 - shift;
   #pragma unroll
       for (int i = 0; i < 8; ++i) x[p][i] = v[p][i] = g[p][i] = 0.f;
       if (c < D) {
-        load_cols((const S*)a.x + n * D, c, D, x[p]);
+        load_part<WHOLE>((const S*)a.x + n * D, c, D, x[p]);
         if (a.v) {
-          load_cols((const B*)a.v + n * D, c, D, v[p]);
-          if (a.gate) load_cols((const B*)a.gate + n * D, c, D, g[p]);
-          load_weight(a.w_after, a.weight_dtype, c, D, w[p]);
+          load_part<WHOLE>((const B*)a.v + n * D, c, D, v[p]);
+          if (a.gate) load_part<WHOLE>((const B*)a.gate + n * D, c, D, g[p]);
+          load_weight<WHOLE>(a.w_after, a.weight_dtype, c, D, w[p]);
         }
       }
     }
@@ -98,18 +127,18 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_kernel(const N
       const float r = a.scale * rsqrtf(ss[0] * inv + a.eps);
   #pragma unroll
       for (int p = 0; p < P; ++p) {
-        const int c = (p * 64 * W + t) * 8;
+        const int c = (p * 64 * W + t) * 8 - shift;
         if (c < D) {
   #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const float s = a.gate ? sigmoid(g[p][i]) : 1.f;
             x[p][i] += s * (w[p][i] * (v[p][i] * r));
           }
-          store_cols((S*)a.y + n * D, c, D, x[p]);
-          if (c + 8 > D)
+          store_part<WHOLE>((S*)a.y + n * D, c, D, x[p]);
+          if (!within<WHOLE>(c, D))
   #pragma unroll
             for (int i = 0; i < 8; ++i)
-              if (c + i >= D) x[p][i] = 0.f;
+              if (c + i < 0 || c + i >= D) x[p][i] = 0.f;
         }
       }
     }
@@ -123,12 +152,12 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_kernel(const N
       const float r = rsqrtf(ss[0] * inv + a.eps);
   #pragma unroll
       for (int p = 0; p < P; ++p) {
-        const int c = (p * 64 * W + t) * 8;
+        const int c = (p * 64 * W + t) * 8 - shift;
         if (c < D) {
-          load_weight(a.w_before, a.weight_dtype, c, D, w[p]);
+          load_weight<WHOLE>(a.w_before, a.weight_dtype, c, D, w[p]);
   #pragma unroll
           for (int i = 0; i < 8; ++i) x[p][i] = w[p][i] * (x[p][i] * r);
-          store_cols((B*)a.u + n * D, c, D, x[p]);
+          store_part<WHOLE>((B*)a.u + n * D, c, D, x[p]);
         }
       }
     }
@@ -140,13 +169,14 @@ template <class T>
 struct Raw {
   typedef T V8 __attribute__((ext_vector_type(8)));
   V8 v;
+  template <bool WHOLE>
   __device__ __forceinline__ void load(const void* row, int c, int D) {
     const T* const p = (const T*)row + c;
-    if (c + 8 <= D) {
+    if (within<WHOLE>(c, D)) {
       __builtin_memcpy(&v, p, sizeof(v));
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = c + i < D ? p[i] : (T)0.f;
+      for (int i = 0; i < 8; ++i) v[i] = c + i >= 0 && c + i < D ? p[i] : (T)0.f;
     }
   }
   __device__ __forceinline__ void clear() {
@@ -159,25 +189,27 @@ struct Raw {
 // W waves a row, weights and their sums in registers: 128 of them where a lane has one group of columns, so that two rows
 // share a CU and the loads of one run beside the sums of the other (8192 rows of 4096 in bf16: 113 us; the next row fetched
 // ahead, with 155 registers and one row a CU, 122).
-template <class S, class B, int W, int P>
-__global__ __launch_bounds__(64 * W, P == 1 ? 4 : 1) void kan_norm_grad_kernel(const NormArgs a, int groups) {
+template <class S, class B, int W, int P, bool WHOLE>
+__global__ __launch_bounds__(64 * W, P == 1 && WHOLE ? 4 : (W == 16 ? 4 : 2)) void kan_norm_grad_kernel(const NormArgs a, int groups) {
   __shared__ float sSum[2][W][3];
   __shared__ float sSum1[2][W][1];
   const int t = threadIdx.x, group = blockIdx.x, D = a.D;
+  const int shift = first_shift<WHOLE, 512 * W * P>(group, D);      // (the same for all rows of the group: it has one, or every 512th)
+  static_assert(kMaxGroups % 8 == 0, "");
   const float inv = 1.f / (float)D;
   float sum1[P][8], sum2[P][8], w1[P][8], w2[P][8];
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    const int c = (p * 64 * W + t) * 8;
+    const int c = (p * 64 * W + t) * 8 - shift;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum1[p][i] = sum2[p][i] = w1[p][i] = w2[p][i] = 0.f;
     if (c < D) {
-      if (a.du) load_weight(a.w_before, a.weight_dtype, c, D, w1[p]);
-      if (a.v) load_weight(a.w_after, a.weight_dtype, c, D, w2[p]);
-      if (c + 8 > D)
+      if (a.du) load_weight<WHOLE>(a.w_before, a.weight_dtype, c, D, w1[p]);
+      if (a.v) load_weight<WHOLE>(a.w_after, a.weight_dtype, c, D, w2[p]);
+      if (!within<WHOLE>(c, D))
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (c + i >= D) w1[p][i] = w2[p][i] = 0.f;
+          if (c + i < 0 || c + i >= D) w1[p][i] = w2[p][i] = 0.f;
     }
   }
   struct Row {
@@ -187,16 +219,16 @@ __global__ __launch_bounds__(64 * W, P == 1 ? 4 : 1) void kan_norm_grad_kernel(c
   auto load = [&](long long n, Row& r) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const int c = (p * 64 * W + t) * 8;
+      const int c = (p * 64 * W + t) * 8 - shift;
       r.y[p].clear(), r.dy[p].clear(), r.du[p].clear(), r.v[p].clear(), r.g[p].clear();
       if (c < D) {
         if (a.du) {
-          r.y[p].load((const S*)a.x + n * D, c, D);
-          r.du[p].load((const B*)a.du + n * D, c, D);
+          r.y[p].template load<WHOLE>((const S*)a.x + n * D, c, D);
+          r.du[p].template load<WHOLE>((const B*)a.du + n * D, c, D);
         }
-        if (a.dy) r.dy[p].load((const S*)a.dy + n * D, c, D);
-        if (a.v) r.v[p].load((const B*)a.v + n * D, c, D);
-        if (a.gate) r.g[p].load((const B*)a.gate + n * D, c, D);
+        if (a.dy) r.dy[p].template load<WHOLE>((const S*)a.dy + n * D, c, D);
+        if (a.v) r.v[p].template load<WHOLE>((const B*)a.v + n * D, c, D);
+        if (a.gate) r.g[p].template load<WHOLE>((const B*)a.gate + n * D, c, D);
       }
     }
   };
@@ -215,7 +247,7 @@ __global__ __launch_bounds__(64 * W, P == 1 ? 4 : 1) void kan_norm_grad_kernel(c
     float sq[1] = {0.f}, q[P][8];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const int c = (p * 64 * W + t) * 8;
+      const int c = (p * 64 * W + t) * 8 - shift;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         q[p][i] = r.dy[p][i];
@@ -225,7 +257,7 @@ __global__ __launch_bounds__(64 * W, P == 1 ? 4 : 1) void kan_norm_grad_kernel(c
           q[p][i] += ry * (r.du[p][i] * w1[p][i] - hat * mean);
         }
       }
-      if (c < D) store_cols((S*)a.dx + n * D, c, D, q[p]);
+      if (c < D) store_part<WHOLE>((S*)a.dx + n * D, c, D, q[p]);
       if (a.v) {
         float dg[8];
 #pragma unroll
@@ -234,9 +266,9 @@ __global__ __launch_bounds__(64 * W, P == 1 ? 4 : 1) void kan_norm_grad_kernel(c
           sum2[p][i] += s * e * m;
           dg[i] = e * (w2[p][i] * m) * (s * (1.f - s));
           q[p][i] = s * e * w2[p][i];
-          sq[0] += c + i < D ? q[p][i] * m : 0.f;
+          sq[0] += q[p][i] * m;
         }
-        if (a.gate && c < D) store_cols((B*)a.dgate + n * D, c, D, dg);
+        if (a.gate && c < D) store_part<WHOLE>((B*)a.dgate + n * D, c, D, dg);
       }
     }
     if (a.v) {
@@ -244,10 +276,10 @@ __global__ __launch_bounds__(64 * W, P == 1 ? 4 : 1) void kan_norm_grad_kernel(c
       const float qm = sq[0] * inv;
 #pragma unroll
       for (int p = 0; p < P; ++p) {
-        const int c = (p * 64 * W + t) * 8;
+        const int c = (p * 64 * W + t) * 8 - shift;
 #pragma unroll
         for (int i = 0; i < 8; ++i) q[p][i] = rv * (q[p][i] - r.v[p][i] * rv * qm);
-        if (c < D) store_cols((B*)a.dv + n * D, c, D, q[p]);
+        if (c < D) store_part<WHOLE>((B*)a.dv + n * D, c, D, q[p]);
       }
     }
   };
@@ -260,10 +292,10 @@ __global__ __launch_bounds__(64 * W, P == 1 ? 4 : 1) void kan_norm_grad_kernel(c
   float* dst = a.partial + (long long)group * D;
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    const int c = (p * 64 * W + t) * 8;
+    const int c = (p * 64 * W + t) * 8 - shift;
     if (c < D) {
-      if (a.dw_before) store_cols(dst, c, D, sum1[p]);
-      if (a.dw_after) store_cols(dst + (a.dw_before ? (long long)groups * D : 0), c, D, sum2[p]);
+      if (a.dw_before) store_part<WHOLE>(dst, c, D, sum1[p]);
+      if (a.dw_after) store_part<WHOLE>(dst + (a.dw_before ? (long long)groups * D : 0), c, D, sum2[p]);
     }
   }
 }
@@ -300,7 +332,8 @@ __global__ __launch_bounds__(kReduceThreads) void kan_norm_reduce_kernel(const f
 // f(W, P): waves per row and groups of eight columns a lane.  Backward a row takes more registers, and more waves.
 template <bool GRAD, class F>
 hipError_t with_shape(int D, F&& f) {
-#define KAN_SHAPE(W, P) if (D <= 512 * W * P) return f(std::integral_constant<int, W>{}, std::integral_constant<int, P>{})
+  const int cols = D + (D % 8 ? 7 : 0);
+#define KAN_SHAPE(W, P) if (cols <= 512 * W * P) return f(std::integral_constant<int, W>{}, std::integral_constant<int, P>{})
   KAN_SHAPE(1, 1);
   if constexpr (GRAD) {
     KAN_SHAPE(2, 1);
@@ -336,7 +369,8 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
     return with_shape<false>(a.D, [&](auto w, auto p) {
       constexpr int W = decltype(w)::value, P = decltype(p)::value;
       const long long blocks = std::min(W == 1 ? (a.N + 3) / 4 : a.N, (long long)kMaxBlocks);
-      hipLaunchKernelGGL((kan_norm_kernel<S, B, W, P>), dim3((unsigned)blocks), dim3(W == 1 ? 256 : 64 * W), 0, s, a);
+      if (a.D % 8 == 0) hipLaunchKernelGGL((kan_norm_kernel<S, B, W, P, true>), dim3((unsigned)blocks), dim3(W == 1 ? 256 : 64 * W), 0, s, a);
+      else hipLaunchKernelGGL((kan_norm_kernel<S, B, W, P, false>), dim3((unsigned)blocks), dim3(W == 1 ? 256 : 64 * W), 0, s, a);
       return hipGetLastError();
     });
   });
@@ -355,7 +389,8 @@ kan_status run_norm_grad(const NormArgs& a, hipStream_t s) {
       typedef decltype(bl) B;
       return with_shape<true>(a.D, [&](auto w, auto p) {
         constexpr int W = decltype(w)::value, P = decltype(p)::value;
-        hipLaunchKernelGGL((kan_norm_grad_kernel<S, B, W, P>), dim3(groups), dim3(64 * W), 0, s, a, groups);
+        if (a.D % 8 == 0) hipLaunchKernelGGL((kan_norm_grad_kernel<S, B, W, P, true>), dim3(groups), dim3(64 * W), 0, s, a, groups);
+        else hipLaunchKernelGGL((kan_norm_grad_kernel<S, B, W, P, false>), dim3(groups), dim3(64 * W), 0, s, a, groups);
         return hipGetLastError();
       });
     });
