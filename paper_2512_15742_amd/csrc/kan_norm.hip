@@ -32,13 +32,27 @@ template <bool WHOLE, int COLS>      // columns that the lanes have
 __device__ __forceinline__ int first_shift(long long n, int D) { return !WHOLE && D + 7 <= COLS ? (int)((n * D) & 7) : 0; }
 template <bool WHOLE>
 __device__ __forceinline__ bool within(int c, int D) { return WHOLE || (c >= 0 && c + 8 <= D); }
+// room: elements from the row's first to the array's end.  A part of eight columns is read with its neighbours in other rows,
+// which are then left out; only at the array's end it is read one by one.
 template <bool WHOLE, class T>
-__device__ __forceinline__ void load_part(const T* row, int c, int D, float (&out)[8]) {
-  if (within<WHOLE>(c, D)) {
+__device__ __forceinline__ void load_part(const T* row, int c, int D, long long room, float (&out)[8]) {
+  if (WHOLE || c + 8 <= room) {
     load8(row + c, out);
+    if (!within<WHOLE>(c, D))
+#pragma unroll
+      for (int i = 0; i < 8; ++i) out[i] = c + i >= 0 && c + i < D ? out[i] : 0.f;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) out[i] = c + i >= 0 && c + i < D ? (float)row[c + i] : 0.f;
+    for (int i = 0; i < 8; ++i) out[i] = c + i < D ? (float)row[c + i] : 0.f;
+  }
+}
+template <bool WHOLE, class T>
+__device__ __forceinline__ void load_vector(const T* w, int c, int D, float (&out)[8]) {
+  if (within<WHOLE>(c, D)) {
+    load8(w + c, out);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] = c + i >= 0 && c + i < D ? (float)w[c + i] : 0.f;
   }
 }
 template <bool WHOLE, class T>
@@ -58,11 +72,11 @@ __device__ __forceinline__ void load_weight(const void* w, int dtype, int c, int
 #pragma unroll
     for (int i = 0; i < 8; ++i) out[i] = 1.f;
   } else if (dtype == KAN_F32) {
-    load_part<WHOLE>((const float*)w, c, D, out);
+    load_vector<WHOLE>((const float*)w, c, D, out);
   } else if (dtype == KAN_F16) {
-    load_part<WHOLE>((const f16*)w, c, D, out);
+    load_vector<WHOLE>((const f16*)w, c, D, out);
   } else {
-    load_part<WHOLE>((const bf16*)w, c, D, out);
+    load_vector<WHOLE>((const bf16*)w, c, D, out);
   }
 }
 
@@ -103,16 +117,17 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_kernel(const N
   for (long long n = W == 1 ? (long long)blockIdx.x * 4 + (threadIdx.x >> 6) : (long long)blockIdx.x; n < a.N; n += rows) {
     float x[P][8], v[P][8], g[P][8], w[P][8];
     const int shift = first_shift<WHOLE, 512 * W * P>(n, D);
+    const long long room = (a.N - n) * D;
   #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int c = (p * 64 * W + t) * 8 - shift;
   #pragma unroll
       for (int i = 0; i < 8; ++i) x[p][i] = v[p][i] = g[p][i] = 0.f;
       if (c < D) {
-        load_part<WHOLE>((const S*)a.x + n * D, c, D, x[p]);
+        load_part<WHOLE>((const S*)a.x + n * D, c, D, room, x[p]);
         if (a.v) {
-          load_part<WHOLE>((const B*)a.v + n * D, c, D, v[p]);
-          if (a.gate) load_part<WHOLE>((const B*)a.gate + n * D, c, D, g[p]);
+          load_part<WHOLE>((const B*)a.v + n * D, c, D, room, v[p]);
+          if (a.gate) load_part<WHOLE>((const B*)a.gate + n * D, c, D, room, g[p]);
           load_weight<WHOLE>(a.w_after, a.weight_dtype, c, D, w[p]);
         }
       }
@@ -170,13 +185,16 @@ struct Raw {
   typedef T V8 __attribute__((ext_vector_type(8)));
   V8 v;
   template <bool WHOLE>
-  __device__ __forceinline__ void load(const void* row, int c, int D) {
+  __device__ __forceinline__ void load(const void* row, int c, int D, long long room) {      // (as load_part)
     const T* const p = (const T*)row + c;
-    if (within<WHOLE>(c, D)) {
+    if (WHOLE || c + 8 <= room) {
       __builtin_memcpy(&v, p, sizeof(v));
+      if (!within<WHOLE>(c, D))
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i >= 0 && c + i < D ? v[i] : (T)0.f;
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = c + i >= 0 && c + i < D ? p[i] : (T)0.f;
+      for (int i = 0; i < 8; ++i) v[i] = c + i < D ? p[i] : (T)0.f;
     }
   }
   __device__ __forceinline__ void clear() {
@@ -223,12 +241,12 @@ __global__ __launch_bounds__(64 * W, P == 1 && WHOLE ? 4 : (W == 16 ? 4 : 2)) vo
       r.y[p].clear(), r.dy[p].clear(), r.du[p].clear(), r.v[p].clear(), r.g[p].clear();
       if (c < D) {
         if (a.du) {
-          r.y[p].template load<WHOLE>((const S*)a.x + n * D, c, D);
-          r.du[p].template load<WHOLE>((const B*)a.du + n * D, c, D);
+          r.y[p].template load<WHOLE>((const S*)a.x + n * D, c, D, (a.N - n) * D);
+          r.du[p].template load<WHOLE>((const B*)a.du + n * D, c, D, (a.N - n) * D);
         }
-        if (a.dy) r.dy[p].template load<WHOLE>((const S*)a.dy + n * D, c, D);
-        if (a.v) r.v[p].template load<WHOLE>((const B*)a.v + n * D, c, D);
-        if (a.gate) r.g[p].template load<WHOLE>((const B*)a.gate + n * D, c, D);
+        if (a.dy) r.dy[p].template load<WHOLE>((const S*)a.dy + n * D, c, D, (a.N - n) * D);
+        if (a.v) r.v[p].template load<WHOLE>((const B*)a.v + n * D, c, D, (a.N - n) * D);
+        if (a.gate) r.g[p].template load<WHOLE>((const B*)a.gate + n * D, c, D, (a.N - n) * D);
       }
     }
   };
