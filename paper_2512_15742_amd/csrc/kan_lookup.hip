@@ -89,15 +89,31 @@ __global__ __launch_bounds__(kRankThreads) void kan_lookup_rank_kernel(const voi
   }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int padded = (N + 63) & ~63;
-  for (int i = threadIdx.x; i < padded; i += kRankThreads) sKey[i] = i < N ? row_of(ids, id_dtype, i, V) : 0xffffffffu;
+#pragma unroll
+  for (int i = 0; i < kRankTokens / kRankThreads; ++i) {
+    const int n = i * kRankThreads + threadIdx.x;
+    if (n < padded) sKey[n] = n < N ? row_of(ids, id_dtype, n, V) : 0xffffffffu;
+  }
   __syncthreads();
   const int mine = blockIdx.x * 64 + lane;       // (blocks are of whole runs of 64: mine < padded)
   const uint32_t key = sKey[mine];
   uint32_t count = 0;
-  const int quads = padded / 4;
-  for (int q = wave; q < quads; q += 16) {
-    const uint4 k = ((const uint4*)sKey)[q];
-    const int at = q * 4;
+  // Tokens in front of the 64: equal keys count; behind: they do not; among them: by position.
+  const int quads = padded / 4, from = blockIdx.x * 16, to = from + 16;
+  const uint4* const k4 = (const uint4*)sKey;
+#pragma unroll 4
+  for (int q = wave; q < from; q += 16) {
+    const uint4 k = k4[q];
+    count += (k.x <= key) + (k.y <= key) + (k.z <= key) + (k.w <= key);
+  }
+#pragma unroll 4
+  for (int q = to + wave; q < quads; q += 16) {
+    const uint4 k = k4[q];
+    count += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
+  }
+  {
+    const uint4 k = k4[from + wave];
+    const int at = (from + wave) * 4;
     count += (k.x < key || (k.x == key && at < mine)) ? 1u : 0u;
     count += (k.y < key || (k.y == key && at + 1 < mine)) ? 1u : 0u;
     count += (k.z < key || (k.z == key && at + 2 < mine)) ? 1u : 0u;
@@ -481,9 +497,10 @@ GradPlan plan_grad(int V, int D, long long N) {
   p.passes = 0;
   if (!p.rank)
     while (p.passes < 4 && ((uint64_t)V >> (kDigitBits * p.passes)) != 0) ++p.passes;       // (V itself is the key of ids that name no row)
-  // Chunks of 32 tokens; of 64 where that leaves 2048 waves busy (fewer rows are written in parts: 66 against 70 us for 16,384
-  // tokens x 4096); longer ones where there would be more than 2^14 of them, so that a run of most tokens has few parts.
-  p.chunk = N / 64 * ((D + 511) / 512) >= 2048 ? 64 : 32;
+  // Chunks of 16 tokens while there are few, so that many waves share them; of 32 and 64 where that leaves 1024 and 2048 waves
+  // busy (fewer rows are written in parts: 66 against 70 us for 16,384 tokens x 4096); longer ones where there would be more
+  // than 2^14 of them, so that a run of most tokens has few parts.
+  p.chunk = N / 64 * ((D + 511) / 512) >= 2048 ? 64 : N / 32 * ((D + 511) / 512) >= 1024 ? 32 : 16;
   while ((N + p.chunk - 1) / p.chunk > (1 << 14)) p.chunk *= 2;
   p.chunks = (N + p.chunk - 1) / p.chunk;
   // Up to 64 columns a lane takes one; wider rows: eight a lane, sixteen-byte loads of 16-bit types.
@@ -566,9 +583,10 @@ kan_status run_lookup_grad(const LookupGradArgs& a, hipStream_t s) {
       long long bytes[2];
       unsigned fb[2];
       for (int k = 0; k < 2; ++k) {
-        const long long from = std::min(fill, (2 * pass + k) * share);
+        const int which = 2 * pass + k;
+        const long long from = std::min(fill, which * share);
         part[k] = (unsigned char*)a.dtable + from;
-        bytes[k] = 2 * pass + k == shares - 1 ? fill - from : std::min(share, fill - from);
+        bytes[k] = which == shares - 1 ? fill - from : std::min(share, fill - from);
         fb[k] = (unsigned)std::min(1024ll, (bytes[k] + 16 * kSortThreads - 1) / (16 * kSortThreads));
       }
       st = run_named("kan_lookup_sort", s, [&] {
