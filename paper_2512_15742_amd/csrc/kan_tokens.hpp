@@ -100,13 +100,8 @@ kan_status run_vocab_grad(const VocabArgs&, hipStream_t);
 // ---- device side ---------------------------------------------------------------------------------------------------
 #if defined(__HIPCC__)
 
-// Eight elements at an address that is aligned to one element: gfx950 takes a 16-byte access at any address, so rows of
-// odd widths need no form of their own.
-template <class T>
-struct alignas(sizeof(T)) __attribute__((packed)) Pack8 {
-  T v[8];
-};
-
+// Eight elements at an address that is aligned to one element: gfx950 takes a 16-byte access at any address, so rows of odd
+// widths need no form of their own.
 template <class T>
 __device__ __forceinline__ void load8(const T* p, float (&out)[8]) {
   typedef T V8 __attribute__((ext_vector_type(8)));

@@ -465,8 +465,9 @@ struct Index {
   float *mul, *factor;
 };
 // What the weights dloss are multiplied with, and what the sums are: fp16 dS has its largest weight at 2^14.
-__device__ __forceinline__ float scale_of(float scale, int half, float top) { return half ? (top > 0.f ? kHalfScale / top : 0.f) : scale; }
-__device__ __forceinline__ float factor_of(float scale, int half, float top) { return half ? scale * (top / kHalfScale) : 1.f; }
+// (A largest weight below 1e-30 is taken for that: its gradients are 0 in fp16, and 2^14 over it would pass fp32.)
+__device__ __forceinline__ float scale_of(float scale, int half, float top) { return half ? kHalfScale / fmaxf(top, 1e-30f) : scale; }
+__device__ __forceinline__ float factor_of(float scale, int half, float top) { return half ? scale * (fmaxf(top, 1e-30f) / kHalfScale) : 1.f; }
 
 __global__ __launch_bounds__(1024) void kan_vocab_index_kernel(const float* __restrict__ dloss, const void* __restrict__ targets, int id_dtype, uint32_t V, int N,
                                                                float scale, int half, const Index x) {
@@ -850,7 +851,7 @@ Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
   limit(1ll << 36, N);
   if (backward) {
     limit(kPieceBytes, p.parts * N * 2);
-    limit(1ll << 36, D);
+    limit(1ll << 35, D);
     limit(1ll << 25, 1);           // (32 rows of dS: 32-bit offsets)
   }
   p.piece = (int)std::min(piece, (long long)INT32_MAX / kVocabStep * kVocabStep);

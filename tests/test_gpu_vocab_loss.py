@@ -68,6 +68,13 @@ def test_both_directions(kb, N, V, D, dtype):
     check_all(kb, *draw(N + V + D, N, V, D, dtype, kind), scale=(1.0, 0.5)[N % 2])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("N,V,D", [(5000, 3001, 72), (4097, 16500, 264), (1500, 9000, 1032)])
+def test_many_tokens(kb, N, V, D, dtype):
+    """Large tiles, long and short contractions, more tokens than a workgroup counts by itself."""
+    check_all(kb, *draw(N + D, N, V, D, dtype, ("i32", "i64", "u16")[N % 3]), scale=1.0)
+
+
 @pytest.mark.parametrize("dtype,N,V,D", [(F16, 40, 50001, 1000), (BF16, 2500, 132000, 64), (F32, 300, 150001, 200)])
 def test_tables_in_several_pieces(kb, dtype, N, V, D):
     check_all(kb, *draw(1, N, V, D, dtype), scale=1.0)
@@ -153,6 +160,10 @@ def test_half_gradients_of_small_and_of_scaled_losses(kb):
     for mul in (1.0, 65536.0 / 64):
         h, table, t, dloss = draw(12, 333, 5000, 64, F16)
         check_all(kb, h, table, t, dloss.sign() / 333 * mul, scale=1.0)
+    _, lse = kb.kan_vocab_loss_forward(h, table, t)
+    for mul in (0.0, 1e-36, 1e-44):               # gradients below the smallest number of fp16: zeros
+        for g in kb.kan_vocab_loss_backward(h, table, t, lse, dloss.sign() * mul):
+            assert not g.any()
 
 
 @pytest.mark.parametrize("dtype", [F32])
