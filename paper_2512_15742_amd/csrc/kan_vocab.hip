@@ -109,8 +109,9 @@ constexpr uint32_t kPartA = 2u | 1u << 2 | 0u << 4 | 1u << 6 | 0u << 8 | 0u << 1
 constexpr uint32_t kPartB = 0u | 1u << 2 | 2u << 4 | 0u << 6 | 1u << 8 | 0u << 10;
 
 // One operand's tile of R rows: a step of it is R x 32 numbers, 64 R bytes of LDS.
-//   k contiguous: [row][4 pieces of 8 k], piece c of row r at place c ^ (r >> 1 & 3), so that eight lanes side by side, which
-//   read one piece of eight rows, meet eight different groups of four banks;
+//   k contiguous: [row][4 pieces of 8 k], piece c of row r at place c ^ (r >> 2 & 3), so that sixteen lanes side by side, which
+//   read one piece of sixteen rows, meet all banks once (c ^ (r >> 1 & 3) does so for eight lanes: half of the clocks of the
+//   LDS were conflicts);
 //   k strided: [k][R / 16 pieces of 16 rows], piece u of row k at place u ^ {0, 2, 5, 7}[k & 3] (R = 64: u ^ (k & 3)): a
 //   transposing read takes one piece of four k in 16 lanes, and two neighbouring ones in 32.
 // The memory pipeline writes LDS in the order of the lanes, so the places are chosen by what each lane asks for.
@@ -137,12 +138,12 @@ struct Tile {
       step = kStep * 2;
       limit = (long long)(min(o.rows - r0, R) - 1) * row + (long long)o.depth * 2;
       const uint32_t l = lane;
-      chunk = (l & 3u) ^ (l >> 3 & 3u);
+      chunk = (l & 3u) ^ (l >> 4 & 3u);
 #pragma unroll
       for (int j = 0; j < kCopies; ++j) off[j] = (uint32_t)((wave * kCopies + j) * 16 + (lane >> 2)) * (uint32_t)row + chunk * 16u;
       chunk *= 8u;
       const uint32_t r = first + (lane & 31);
-      read = r * 64u + ((uint32_t)(lane >> 5) ^ (r >> 1 & 3u)) * 16u;
+      read = r * 64u + ((uint32_t)(lane >> 5) ^ (r >> 2 & 3u)) * 16u;
     } else {
       base = (const char*)o.p + (long long)r0 * 2;
       step = kStep * row;
