@@ -751,20 +751,28 @@ __global__ __launch_bounds__(kThreads) void kan_vocab_round_kernel(const float* 
 constexpr int kCus = 256;
 enum TileKind : int { k256x256, k256x128, k256x64, k128x64, kTileKinds };
 constexpr int kTileM[] = {256, 256, 256, 128}, kTileN[] = {256, 128, 64, 64};
-// Workgroups that share a CU, ns of a step of 32 with all of them on it, and ns of a tile's beginning and end: with the
-// statistics of z, and with rows that leave through LDS (measured on products of 8192 x 131072 x 2048, 1111 x 50021 x 1000 and
-// 16 x 65536 x 2048).
-constexpr long long kPerCu[] = {1, 2, 2, 3}, kStepNs[] = {850, 1040, 660, 560};
-constexpr long long kStatNs[] = {5000, 4000, 4500, 4000}, kRowsNs[] = {13000, 8000, 5800, 4300};
+// Workgroups that fit a CU, and ns of a step of 32 and of a tile's beginning and end, with that many on it and with one: with the
+// statistics of z, and with rows that leave through LDS (measured on products of 8192 x 131072 x 2048, 2000 x 32000 x 1024,
+// 1111 x 50021 x 1000 and 500 x 10007 x 1536).
+constexpr long long kPerCu[] = {1, 2, 2, 3};
+struct Cost {
+  long long step, stats, rows;
+};
+constexpr Cost kFull[] = {{830, 5000, 15000}, {915, 7500, 11000}, {590, 9000, 6500}, {500, 6000, 4500}};
+constexpr Cost kAlone[] = {{830, 5000, 13000}, {420, 4500, 8000}, {330, 4500, 6000}, {245, 4000, 4300}};
 
 long long tiles_of(int kind, long long m, long long n) { return ((m + kTileM[kind] - 1) / kTileM[kind]) * ((n + kTileN[kind] - 1) / kTileN[kind]); }
 long long steps_of(long long k, int parts) { return (k + kStep - 1) / kStep * (parts == 1 ? 1 : 6); }
-long long tile_ns(int kind, long long steps, bool stats) { return steps * kStepNs[kind] + (stats ? kStatNs : kRowsNs)[kind]; }
-
-// ns until the fullest CU is done.  (A round that is not full has fewer workgroups a CU, which are faster then.)
-long long rounds_ns(int kind, long long tiles, long long each) {
-  const long long full = tiles / (kCus * kPerCu[kind]), rest = tiles % (kCus * kPerCu[kind]);
-  return full * each + (rest ? each * ((rest + kCus - 1) / kCus + 1) / (kPerCu[kind] + 1) : 0);
+// of a tile with `on` workgroups on its CU
+long long tile_ns(int kind, long long steps, bool stats, long long on) {
+  const Cost &f = kFull[kind], &a = kAlone[kind];
+  const long long full = steps * f.step + (stats ? f.stats : f.rows), alone = steps * a.step + (stats ? a.stats : a.rows);
+  return kPerCu[kind] == 1 ? full : alone + (full - alone) * (on - 1) / (kPerCu[kind] - 1);
+}
+// until the last of `tiles` is done
+long long rounds_ns(int kind, long long tiles, long long steps, bool stats) {
+  const long long slots = kCus * kPerCu[kind], rest = tiles % slots;
+  return tiles / slots * tile_ns(kind, steps, stats, kPerCu[kind]) + (rest ? tile_ns(kind, steps, stats, (rest + kCus - 1) / kCus) : 0);
 }
 
 // The tiles that are done first.
@@ -772,7 +780,7 @@ int pick_tiles(long long m, long long n, long long steps, bool stats) {
   int best = 0;
   long long least = -1;
   for (int kind = 0; kind < kTileKinds; ++kind) {
-    const long long c = rounds_ns(kind, tiles_of(kind, m, n), tile_ns(kind, steps, stats));
+    const long long c = rounds_ns(kind, tiles_of(kind, m, n), steps, stats);
     if (least < 0 || c < least) {
       least = c;
       best = kind;
@@ -785,13 +793,15 @@ int pick_tiles(long long m, long long n, long long steps, bool stats) {
 // each adds a slice of N x D sums that is written and read once.
 void pick_grads(long long N, long long V, long long D, int parts, int* kind, int* slices) {
   long long least = -1;
-  const long long steps = steps_of(V, parts);
+  const long long steps = steps_of(V, parts), table_steps = steps_of(N, parts);
   for (int k = 0; k < kTileKinds; ++k)
     for (int s = 1; s <= 32 && (s == 1 || steps / s >= 8); ++s) {
-      const long long rows = tile_ns(k, (steps + s - 1) / s, false), table = tile_ns(k, steps_of(N, parts), false);
-      const long long n1 = tiles_of(k, D, N) * s, n2 = tiles_of(k, D, V), slots = kCus * kPerCu[k];
-      // dh's rounds, or the CUs' work in all and the end of the last tiles, which are dT's
-      long long c = std::max((n1 + slots - 1) / slots * rows, n1 + n2 > slots ? (n1 * rows + n2 * table) / slots + table / 2 : std::max(rows, table));
+      const long long n1 = tiles_of(k, D, N) * s, n2 = tiles_of(k, D, V), slots = kCus * kPerCu[k], row_steps = (steps + s - 1) / s;
+      const long long on = std::min(kPerCu[k], (n1 + n2 + kCus - 1) / kCus);
+      const long long rows = tile_ns(k, row_steps, false, on), table = tile_ns(k, table_steps, false, on);
+      // the longest, if all have a place at once; else dh's rounds, or the CUs' work in all and the end of the last tiles, dT's
+      long long c = std::max(rows, table);
+      if (n1 + n2 > slots) c = std::max((n1 + slots - 1) / slots * rows, (n1 * rows + n2 * table) / slots + tile_ns(k, table_steps, false, 1) / 2);
       c += N * D * 8 * (s - 1) / 4000;
       if (least < 0 || c < least) {
         least = c;
