@@ -12,6 +12,11 @@
 // the histogram of the ids: a chunk sums its runs in fp32, writes the rows of runs that lie within it, and leaves what
 // a run has in it when the run goes on in another chunk; a last launch joins those parts in their order.  So a token
 // that is a tenth of a batch costs no more than others.
+//
+// Measured, and the bytes at a large copy's 5.1 TB/s: 16,384 tokens of 4,096 columns, bf16 table, fp32 rows 86 us (78); gradient of a
+// table of 65,536 such rows 167 us (105): 98 for the sort, beside which the rows that no token names are written as zeros,
+// 66 for the sums, 3 for the joining; gradient of 65,536 rows of ten columns from 1,048,576 edges 80 us (9): 42 for the sort,
+// whose launches follow one another, 28 for the sums, 12 for the joining.
 #include <algorithm>
 #include <type_traits>
 

@@ -9,8 +9,8 @@
 //   dw_before = sum du y ry,   dw_after = sum scale s gy m     (over the tokens)
 //
 // Bound by the bytes of the rows: each is read once, a row stays in the registers of one to sixteen waves, eight columns a
-// lane at a time (8192 rows of 2048 in bf16 with fp32 blocks and gates forward 53 us, 5.0 TB/s; of 4096 in bf16 backward 113 us,
-// 4.7 TB/s; a large copy reaches 5.1).  Norms, means and the sums of the weights' gradients are fp32.  The u of the forward pass is formed from
+// lane at a time (8192 rows of 2048 in bf16 with fp32 blocks and gates forward 49 us, 5.4 TB/s; of 4096 in bf16 backward 111 us,
+// 4.8 TB/s; a large copy reaches 5.1).  Norms, means and the sums of the weights' gradients are fp32.  The u of the forward pass is formed from
 // the fp32 y, not from its rounded copy.  Backward: up to 512 groups of waves take rows in turn and keep the sums of their
 // rows' weight gradients in registers; a second launch adds the groups' sums in a fixed order.
 #include <algorithm>
@@ -205,7 +205,7 @@ struct Raw {
 };
 
 // W waves a row, weights and their sums in registers: 128 of them where a lane has one group of columns, so that two rows
-// share a CU and the loads of one run beside the sums of the other (8192 rows of 4096 in bf16: 113 us; the next row fetched
+// share a CU and the loads of one run beside the sums of the other (8192 rows of 4096 in bf16: 111 us; the next row fetched
 // ahead, with 155 registers and one row a CU, 122).
 template <class S, class B, int W, int P, bool WHOLE>
 __global__ __launch_bounds__(64 * W, P == 1 && WHOLE ? 4 : (W == 16 ? 4 : 2)) void kan_norm_grad_kernel(const NormArgs a, int groups) {

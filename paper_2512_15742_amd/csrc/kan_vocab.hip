@@ -5,13 +5,20 @@
 //   dh = dS T,   dT (+)= dS^t h
 //
 // Forward: tiles of z stay in registers; each leaves the maximum and the sum of exponentials of its part of a row, which a
-// small launch joins.  Backward: piece by piece of the table, z again, dS of the piece in the workspace, and two products
-// with it.  All products run on the matrix cores with fp32 sums.
+// small launch joins.  Backward: piece by piece of the table (z formed once more: dS of 8,192 x 131,072 tokens and rows would
+// be 2.1 GB, pieces of 256 MiB take 1.5 % longer than all of it), dS of the piece in the workspace, and two products with it.
+// All products run on the matrix cores with fp32 sums.
 //
-// Operands are 16-bit numbers.  fp32 rows travel as three bf16 parts (24 bits together; 8 of the smaller parts' products
-// are below 2^-24 of the whole and left out), so a product is six of parts.  dS of 16-bit types is rounded to the type (2^-9 or 2^-12
-// of each entry, the step of the gradients themselves): its entries are about as far apart as the logits, and fp16 holds
-// them times 2^14 / max |dloss|, so that probabilities down to 4e-9 keep all bits.
+// Operands are 16-bit numbers.  fp32 rows travel as three bf16 parts (24 bits together; of the nine products of parts the three
+// that are at most 2^-24 of the whole are left out), so a product is six of parts.  dS of 16-bit types is rounded to the type (at
+// most 2^-8 or 2^-11 of each entry, the step of the gradients themselves).  It is held in units of max |dloss|, so that the equal
+// weights of a mean are not all off by the same rounding (1/255 by 2^-8.01, and all gradients with it); fp16 in 2^-14 of that, so that
+// probabilities down to 4e-9 keep all bits.
+//
+// Bound: few tokens by the bytes of the table (one token x 65,536 x 2,048 in bf16 51 us, 5.3 TB/s); many by the matrix cores and
+// the power that they draw (8,192 x 131,072 x 2,048: the loss 3.6 ms, 1.21 PFLOP/s; loss and gradients 15.0 ms, 1.17 PFLOP/s over
+// four products; the clock falls to 1.7 GHz, matrix units busy 62 % of it in the loss, 50 % with dS, 69 % in the
+// gradients).  Between, launches and tiles that do not fill the CUs (500 x 10,007 x 256 in fp32 123 us in seven launches).
 #include <float.h>
 
 #include <algorithm>
@@ -33,7 +40,7 @@ constexpr int kStep = 32;               // products along the contraction per st
 constexpr int kVocabStep = 256;         // pieces of the table are multiples of it
 constexpr long long kPackBytes = 256ll << 20, kPieceBytes = 256ll << 20;
 
-constexpr float kHalfScale = 16384.f;   // of fp16 dS
+constexpr float kHalfUnit = 16384.f;    // the largest weight of fp16 dS
 
 template <class T>
 __device__ __forceinline__ f32x16 mfma(uint4 a, uint4 b, f32x16 c) {
@@ -459,19 +466,22 @@ __global__ __launch_bounds__(kThreads, waves_of(S::kLds)) void kan_vocab_grads_k
 }
 
 // Which tokens have a target that names a row: their numbers in order, from the back of the list those of the others; how
-// many; fp16: what dS is multiplied with so that the largest weight is 2^14, and the factor that takes this back.
+// many; what their weights are multiplied with, and the factor that takes this back.
 struct Index {
   int* list;                 // [N]
   int* count;
   float *mul, *factor;
 };
-// What the weights dloss are multiplied with, and what the sums are: fp16 dS has its largest weight at 2^14.
-// (A largest weight below 1e-30 is taken for that: its gradients are 0 in fp16, and 2^14 over it would pass fp32.)
-__device__ __forceinline__ float scale_of(float scale, int half, float top) { return half ? kHalfScale / fmaxf(top, 1e-30f) : scale; }
-__device__ __forceinline__ float factor_of(float scale, int half, float top) { return half ? scale * (fmaxf(top, 1e-30f) / kHalfScale) : 1.f; }
+// What the weights dloss are multiplied with, and the sums after it: the largest weight `top` is at `unit` (0: as it is).
+// (Weights below 1e-30 and above 2^126 are not brought there, so that nothing here leaves fp32's range.)
+__device__ __forceinline__ float within_fp32(float top) { return fminf(fmaxf(top, 1e-30f), 0x1p126f); }
+__device__ __forceinline__ float scale_of(float scale, float unit, float top) { return unit != 0.f ? unit / within_fp32(top) : scale; }
+__device__ __forceinline__ float factor_of(float scale, float unit, float top) { return unit != 0.f ? scale * (within_fp32(top) / unit) : 1.f; }
+// (infinite and NaN weights spoil their own rows alone)
+__device__ __forceinline__ float larger(float top, float dloss) { return fabsf(dloss) <= FLT_MAX ? fmaxf(top, fabsf(dloss)) : top; }
 
 __global__ __launch_bounds__(1024) void kan_vocab_index_kernel(const float* __restrict__ dloss, const void* __restrict__ targets, int id_dtype, uint32_t V, int N,
-                                                               float scale, int half, const Index x) {
+                                                               float scale, float unit, const Index x) {
   __shared__ int sCount[16];
   __shared__ float sMax[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -491,7 +501,7 @@ __global__ __launch_bounds__(1024) void kan_vocab_index_kernel(const float* __re
     at += __popcll(all & ((1ull << lane) - 1));
     if (named) {
       x.list[at] = n;
-      if (half) top = fmaxf(top, fabsf(dloss[n]));
+      if (unit != 0.f) top = larger(top, dloss[n]);
     } else if (n < N) {
       x.list[N - 1 - (n - at)] = n;
     }
@@ -504,8 +514,8 @@ __global__ __launch_bounds__(1024) void kan_vocab_index_kernel(const float* __re
   if (threadIdx.x != 0) return;
   *x.count = before;
   for (int w = 0; w < 16; ++w) top = fmaxf(top, sMax[w]);
-  *x.mul = scale_of(scale, half, top);
-  *x.factor = factor_of(scale, half, top);
+  *x.mul = scale_of(scale, unit, top);
+  *x.factor = factor_of(scale, unit, top);
 }
 
 // Rows in the form the products take: 16-bit parts of `width` columns (zeros behind the last).
@@ -554,8 +564,8 @@ struct TokenArgs {
   Index x;
   int N, D, width, id_dtype;
   uint32_t V;
-  float scale;
-  int half, own_index;
+  float scale, unit;
+  int own_index;
   unsigned blocks;
   PackArgs table;            // and rows of the table by the workgroups behind
 };
@@ -599,7 +609,7 @@ __global__ __launch_bounds__(kThreads) void kan_vocab_tokens_kernel(const TokenA
     if (row_of(a.targets, a.id_dtype, n, a.V) < a.V) {
       ++all;
       front += n < first ? 1 : 0;
-      if (a.half) top = fmaxf(top, fabsf(a.dloss[n]));
+      if (a.unit != 0.f) top = larger(top, a.dloss[n]);
     }
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) {
@@ -616,10 +626,10 @@ __global__ __launch_bounds__(kThreads) void kan_vocab_tokens_kernel(const TokenA
   front = sFront[0] + sFront[1] + sFront[2] + sFront[3];
   all = sAll[0] + sAll[1] + sAll[2] + sAll[3];
   top = fmaxf(fmaxf(sMax[0], sMax[1]), fmaxf(sMax[2], sMax[3]));
-  const float mul = scale_of(a.scale, a.half, top);
+  const float mul = scale_of(a.scale, a.unit, top);
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     *a.x.count = all;
-    *a.x.factor = factor_of(a.scale, a.half, top);
+    *a.x.factor = factor_of(a.scale, a.unit, top);
   }
   const int n = first + wave;           // a wave has a token
   if (n >= a.N) return;
@@ -979,16 +989,17 @@ kan_status run_vocab_grad(const VocabArgs& a, hipStream_t s) {
   const int N = (int)a.N;
   const Index x = {(int*)(ws + p.list), (int*)(ws + p.scalars), (float*)(ws + p.scalars) + 1, (float*)(ws + p.scalars) + 2};
   const bool own_index = N <= kOwnIndex;
+  const float unit = a.dtype == KAN_F32 ? 0.f : a.dtype == KAN_F16 ? kHalfUnit : 1.f;
   kan_status st = KAN_OK;
   if (!own_index) {
     st = run_named("kan_vocab_index", s, [&] {
-      hipLaunchKernelGGL(kan_vocab_index_kernel, dim3(1), dim3(1024), 0, s, a.dloss, a.targets, a.id_dtype, (uint32_t)a.V, N, a.scale, a.dtype == KAN_F16, x);
+      hipLaunchKernelGGL(kan_vocab_index_kernel, dim3(1), dim3(1024), 0, s, a.dloss, a.targets, a.id_dtype, (uint32_t)a.V, N, a.scale, unit, x);
       return hipGetLastError();
     });
     if (st != KAN_OK) return st;
   }
   TokenArgs ta = {a.h, a.targets, a.lse, a.dloss, ws + p.h, a.dh, (int*)(ws + p.target), (float*)(ws + p.lse), (float*)(ws + p.weight), x, N, a.D, (int)p.width,
-                  a.id_dtype, (uint32_t)a.V, a.scale, a.dtype == KAN_F16, own_index, 0, {}};
+                  a.id_dtype, (uint32_t)a.V, a.scale, unit, own_index, 0, {}};
   ta.blocks = own_index ? (unsigned)(N + kTokensPerBlock - 1) / kTokensPerBlock : item_blocks(N * (p.width / 8));
   return with_operand(a.dtype, [&](auto t) -> kan_status {
     typedef decltype(t) T;

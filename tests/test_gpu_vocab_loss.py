@@ -166,6 +166,37 @@ def test_half_gradients_of_small_and_of_scaled_losses(kb):
             assert not g.any()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("N", [255, 255 * 32])
+def test_gradients_of_a_mean_are_not_all_too_large(kb, N, dtype):
+    """1 / N is off by 2^-8.01 in bf16.  A target's entry is (p - 1) / N, p at 2^-13 in the mean: off by that in units of 1 / N.  The
+    errors of the others and of the results are independent, 2^-8 / sqrt(N D) together at most."""
+    g = torch.Generator(device="cuda").manual_seed(21)
+    V, D = 8192, 64
+    table = (torch.randn((V, D), generator=g, device="cuda") / D ** 0.5).to(dtype)
+    h = torch.randn((N, D), generator=g, device="cuda").to(dtype)
+    t = torch.randint(0, V, (N,), generator=g, device="cuda")
+    dloss = torch.full((N,), 1.0 / N, device="cuda")
+    _, lse = kb.kan_vocab_loss_forward(h, table, t)
+    for got, (want, _, _) in zip(kb.kan_vocab_loss_backward(h, table, t, lse, dloss), Loss(h, table, t, 1.0).grads(dloss)):
+        assert abs(float((got.double() * want).sum() / want.square().sum()) - 1) < 2.0 ** -10
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("N", [70, 4200])
+def test_weights_that_are_no_numbers_stay_in_their_rows(kb, N, dtype):
+    h, table, t, dloss = draw(22, N, 300, 64, dtype, left_out=0.0)
+    _, lse = kb.kan_vocab_loss_forward(h, table, t)
+    clean = dloss.clone()
+    for row, value in ((3, float("inf")), (5, float("nan")), (N - 1, -float("inf"))):
+        clean[row] = 0.0
+        dloss[row] = value
+    keep = torch.isfinite(dloss)
+    dh, _ = kb.kan_vocab_loss_backward(h, table, t, lse, dloss)
+    assert torch.equal(dh[keep], kb.kan_vocab_loss_backward(h, table, t, lse, clean)[0][keep])
+    assert not torch.isfinite(dh[~keep]).any()
+
+
 @pytest.mark.parametrize("dtype", [F32])
 def test_gradients_are_differences(kb, dtype):
     h, table, t, dloss = draw(14, 30, 200, 24, dtype)
