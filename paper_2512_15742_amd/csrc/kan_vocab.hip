@@ -465,6 +465,178 @@ __global__ __launch_bounds__(kThreads, waves_of(S::kLds)) void kan_vocab_grads_k
   else product<T, false, false, kGradTable, S>(table, blockIdx.x - row_blocks, sRing);
 }
 
+// ---- few tokens, fp32 -------------------------------------------------------------------------------------------------
+// The table is read as it is, three times for loss and gradients, and split into its parts in registers; the parts in the
+// workspace are one and a half times its bytes, written twice and read three times, by tiles whose steps are six times as many.
+// NB blocks of 32 tokens; the product of the first parts and the smaller ones have sums of their own.  Bound by the reads of the
+// table, from two blocks on by those of the tokens' parts out of L2.  Loss and gradients, with parts in the workspace and so (us):
+// 6 x 83,911 x 2,952 3,308 and 1,028 (z 3.4 to 4.3 TB/s), 18 x 81,628 x 128 173 and 93, 20 x 2,000 x 256 50 and 38,
+// 38 x 9,283 x 1,984 300 and 194, 64 x 30,000 x 1,024 329 and 293; four blocks: 65 x 30,000 x 1,024 386 and 402.
+template <int NB>
+struct FewSums {
+  f32x16 high[NB], low[NB];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) high[j][i] = low[j][i] = 0.f;
+  }
+  // v: eight k of a row of A; b: rows of B, their parts `part` further
+  __device__ __forceinline__ void add(float (&v)[8], const bf16* const (&b)[NB], long long k, long long part) {
+    uint4 a[3];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      bf16x8 t;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        t[i] = (bf16)v[i];
+        v[i] -= (float)t[i];
+      }
+      a[p] = __builtin_bit_cast(uint4, t);
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      uint4 w[3];
+#pragma unroll
+      for (int p = 0; p < 3; ++p) w[p] = *(const uint4*)(b[j] + p * part + k);
+      low[j] = mfma<bf16>(a[2], w[0], low[j]);
+      low[j] = mfma<bf16>(a[1], w[1], low[j]);
+      low[j] = mfma<bf16>(a[0], w[2], low[j]);
+      low[j] = mfma<bf16>(a[1], w[0], low[j]);
+      low[j] = mfma<bf16>(a[0], w[1], low[j]);
+      high[j] = mfma<bf16>(a[0], w[0], high[j]);
+    }
+  }
+};
+
+// z of 32 rows of the table: four waves share the columns, 64 at a time, and add their sums through LDS.
+constexpr int kFewRows = 32;
+template <int EPI, int NB>
+__global__ __launch_bounds__(kThreads) void kan_vocab_few_kernel(const ProductArgs g) {
+  __shared__ float sSum[4][16][64];
+  __shared__ float2 sStat[4][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ln = lane & 31, lh = lane >> 5;
+  const int n_here = g.count ? min(g.n, *g.count) : g.n, m0 = (int)blockIdx.x * kFewRows;
+  if (n_here == 0) return;
+  const float* const row = (const float*)g.a.p + (long long)min(m0 + ln, g.m - 1) * g.a.stride;
+  const bf16* b[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) b[j] = (const bf16*)g.b.p + (long long)min(32 * j + ln, n_here - 1) * g.b.stride;
+  FewSums<NB> sums;
+  sums.clear();
+  for (int k0 = wave * 64; k0 < g.k; k0 += 256) {
+    float v[4][8];
+    if (k0 + 64 <= g.k) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) load8(row + k0 + 16 * h + 8 * lh, v[h]);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 4; ++h)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int k = k0 + 16 * h + 8 * lh + i;
+          v[h][i] = k < g.k ? row[k] : 0.f;
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 4; ++h) sums.add(v[h], b, k0 + 16 * h + 8 * lh, g.b.part);      // (zeros behind B's last column)
+  }
+  const float scale = g.scale * 1.44269504088896f;
+  const int m = 8 * wave + 4 * lh, rows = g.m - m0 - m;       // the lane's four rows of token ln
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const int n = 32 * j + ln;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sSum[wave][i][lane] = sums.high[j][i] + sums.low[j][i];
+    __syncthreads();
+    float z[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) z[q] = (sSum[0][4 * wave + q][lane] + sSum[1][4 * wave + q][lane]) + (sSum[2][4 * wave + q][lane] + sSum[3][4 * wave + q][lane]);
+    if constexpr (EPI == kStats) {
+      float top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        z[q] = q < rows ? z[q] * scale : -INFINITY;
+        top = fmaxf(top, z[q]);
+      }
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float at = fminf(fmaxf(top, -FLT_MAX), FLT_MAX);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sum += __builtin_amdgcn_exp2f(z[q] - at);
+      sum += __shfl_xor(sum, 32);
+      if (lh == 0) sStat[wave][ln] = make_float2(at, sum);
+      __syncthreads();
+      if (threadIdx.x < 32 && n < g.n) {
+        float all = sStat[0][ln].x, total = 0.f;
+#pragma unroll
+        for (int w = 1; w < 4; ++w) all = fmaxf(all, sStat[w][ln].x);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) total += sStat[w][ln].y * __builtin_amdgcn_exp2f(sStat[w][ln].x - all);
+        g.stats[(long long)((g.v0 + m0) / kFewRows) * g.n + n] = make_float2(all, total);
+      }
+    } else {
+      if (n < n_here) {
+        const float lse = g.lse[n] * 1.44269504088896f, weight = g.weight[n];
+        const int hit = g.targets[n] - g.v0 - m0 - m;
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(z[q], scale, -lse));
+          v[q] = q < rows ? (q == hit ? e - 1.f : e) * weight : 0.f;
+        }
+        bf16* dst = (bf16*)g.ds + n * g.ds_stride + m0 + m;
+#pragma unroll
+        for (int p = 0; p < 3; ++p, dst += g.ds_part) {
+          typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+          bf16x4 t;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            t[q] = (bf16)v[q];
+            v[q] -= (float)t[q];
+          }
+          *(bf16x4*)dst = t;
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// dh's slices: four waves take 32 columns each of the same rows of the table.
+template <int NB>
+__global__ __launch_bounds__(kThreads) void kan_vocab_few_rows_kernel(const ProductArgs g) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ln = lane & 31, lh = lane >> 5;
+  const int n_here = min(g.n, *g.count), d0 = (int)blockIdx.x * 128 + wave * 32, split = blockIdx.y;
+  if (n_here == 0 || d0 >= g.m) return;
+  const float* const column = (const float*)g.a.p + min(d0 + ln, g.m - 1);
+  const bf16* b[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) b[j] = (const bf16*)g.b.p + (long long)min(32 * j + ln, n_here - 1) * g.b.stride;
+  FewSums<NB> sums;
+  sums.clear();
+  const long long steps = (g.k + 31) / 32;
+  const int s0 = (int)(steps * split / g.splits), s1 = (int)(steps * (split + 1) / g.splits);
+  for (int s = s0; s < s1; ++s) {
+    float v[2][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[h][i] = column[(long long)min(32 * s + 16 * h + 8 * lh + i, g.k - 1) * g.a.stride];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) sums.add(v[h], b, 32 * s + 16 * h + 8 * lh, g.b.part);       // (dS is zero behind the last row)
+  }
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const int n = 32 * j + ln;
+    float* const out = (float*)g.out + split * g.out_slice + n * g.out_stride;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int d = d0 + 8 * (i >> 2) + 4 * lh + (i & 3);
+      if (n < n_here && d < g.m) out[d] = sums.high[j][i] + sums.low[j][i] + (g.add ? out[d] : 0.f);
+    }
+  }
+}
+
 // Which tokens have a target that names a row: their numbers in order, from the back of the list those of the others; how
 // many; what their weights are multiplied with, and the factor that takes this back.
 struct Index {
@@ -849,20 +1021,45 @@ hipError_t launch_grads(const ProductArgs& rows, const ProductArgs& table, int k
   });
 }
 
+// f(NB{}) for the blocks of 32 of n tokens.
+constexpr int kFewTokens = 64;
+template <class F>
+hipError_t with_blocks(long long n, F&& f) {
+  if (n <= 32) return f(std::integral_constant<int, 1>{});
+  return f(std::integral_constant<int, 2>{});
+}
+template <int EPI>
+hipError_t launch_few(const ProductArgs& g, hipStream_t s) {
+  return with_blocks(g.n, [&](auto nb) {
+    hipLaunchKernelGGL((kan_vocab_few_kernel<EPI, decltype(nb)::value>), dim3((unsigned)(g.m + kFewRows - 1) / kFewRows), dim3(kThreads), 0, s, g);
+    return hipGetLastError();
+  });
+}
+hipError_t launch_few_rows(const ProductArgs& g, hipStream_t s) {
+  return with_blocks(g.n, [&](auto nb) {
+    hipLaunchKernelGGL((kan_vocab_few_rows_kernel<decltype(nb)::value>), dim3((unsigned)(g.m + 127) / 128, (unsigned)g.splits), dim3(kThreads), 0, s, g);
+    return hipGetLastError();
+  });
+}
+
 struct Plan {
   int parts;
-  bool pack_table;            // the table's rows go through the workspace
+  bool few;                   // fp32 tokens that do not make it worth to write the table's parts
+  bool pack_table, pack_rows; // the table's rows, h go through the workspace
   long long width;            // columns of packed rows
   int piece, pieces;          // rows of the table that are dealt with at a time
   int slices;                 // of dh
-  int z_kind, grad_kind;      // tiles of z, of dh and dT
+  int z_kind, grad_kind;      // tiles of z, of dh and dT (few: of dT)
+  int stat_rows;              // of the table that share statistics
   size_t h, table, stats, list, target, lse, weight, scalars, ds, dh, bytes;
 };
 
 Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
   Plan p = {};
   p.parts = dtype == KAN_F32 ? 3 : 1;
-  p.pack_table = p.parts > 1 || D % 8 != 0;
+  p.few = dtype == KAN_F32 && N <= kFewTokens;
+  p.pack_table = !p.few && (p.parts > 1 || D % 8 != 0);
+  p.pack_rows = p.few || p.pack_table;
   p.width = ((long long)D + 63) / 64 * 64;
   const long long all = ((long long)V + kVocabStep - 1) / kVocabStep * kVocabStep;
   long long piece = all;
@@ -878,17 +1075,22 @@ Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
   p.piece = (int)std::min(piece, (long long)INT32_MAX / kVocabStep * kVocabStep);
   p.pieces = (int)((V + (long long)p.piece - 1) / p.piece);
   p.z_kind = pick_tiles(std::min(p.piece, V), N, steps_of(D, p.parts), !backward);
+  p.stat_rows = p.few ? kFewRows : kTileM[p.z_kind];
   if (backward) pick_grads(N, std::min(p.piece, V), D, p.parts, &p.grad_kind, &p.slices);
+  if (p.few) {       // four workgroups a CU (two blocks of tokens: two, 64 x 30,000 x 1,024 296 against 317 us), with 64 rows of the table each or more
+    p.grad_kind = pick_tiles(D, std::min(p.piece, V), steps_of(N, p.parts), false);
+    p.slices = (int)std::max(1ll, std::min({256ll, (N > 32 ? 2ll : 4ll) * kCus / ((D + 127) / 128), (long long)std::min(p.piece, V) / 64}));
+  }
   size_t at = 0;
   auto take = [&](long long bytes) {
     const size_t was = at;
     at += (size_t)(bytes + 255) / 256 * 256;
     return was;
   };
-  p.h = take(backward || p.pack_table ? p.parts * N * p.width * 2 : 0);
+  p.h = take(backward || p.pack_rows ? p.parts * N * p.width * 2 : 0);
   p.table = take(p.pack_table ? p.parts * (long long)p.piece * p.width * 2 : 0);
   if (!backward) {
-    p.stats = take(all / kTileM[p.z_kind] * N * 8);
+    p.stats = take(all / p.stat_rows * N * 8);
   } else {
     p.list = take(N * 4);
     p.target = take(N * 4);
@@ -958,21 +1160,21 @@ kan_status run_vocab_loss(const VocabArgs& a, hipStream_t s) {
     g.scale = a.scale;
     g.stats = (float2*)(ws + p.stats);
     kan_status st;
-    g.b = p.pack_table ? Operand{ws + p.h, p.width, a.N * p.width, (int)a.N, (int)p.width} : Operand{a.h, a.D, 0, (int)a.N, a.D};
+    g.b = p.pack_rows ? Operand{ws + p.h, p.width, a.N * p.width, (int)a.N, (int)p.width} : Operand{a.h, a.D, 0, (int)a.N, a.D};
     for (int v0 = 0, i = 0; i < p.pieces; ++i, v0 += p.piece) {
       PackArgs job;
       g.v0 = v0;
       g.m = std::min(p.piece, a.V - v0);
       g.a = table_rows(a, p, ws, v0, g.m, &job);
-      if (p.pack_table) {
+      if (p.pack_table || (p.pack_rows && i == 0)) {
         const PackArgs rows = {a.h, ws + p.h, i == 0 ? a.N : 0};
         if ((st = pack(job, rows, a.D, p.width, a.dtype, s)) != KAN_OK) return st;
       }
-      st = run_named("kan_vocab_loss", s, [&] { return launch_product<T, kStats>(g, p.z_kind, s); });
+      st = run_named("kan_vocab_loss", s, [&] { return p.few ? launch_few<kStats>(g, s) : launch_product<T, kStats>(g, p.z_kind, s); });
       if (st != KAN_OK) return st;
     }
     return run_named("kan_vocab_join", s, [&] {
-      const int rows = kTileM[p.z_kind];
+      const int rows = p.stat_rows;
       const JoinArgs j = {g.stats, a.h, a.table, a.targets, a.loss, a.lse, (a.V + rows - 1) / rows, (int)a.N, a.D, a.id_dtype, (uint32_t)a.V, a.scale};
       return with_float(a.dtype, [&](auto i) {
         if (a.N <= 1024) hipLaunchKernelGGL((kan_vocab_join_kernel<decltype(i), 1>), dim3((unsigned)a.N), dim3(256), 0, s, j);
@@ -1040,7 +1242,7 @@ kan_status run_vocab_grad(const VocabArgs& a, hipStream_t s) {
       g.k = a.D;
       g.a = table;
       g.b = h;
-      st = run_named("kan_vocab_ds", s, [&] { return launch_product<T, kGradS>(g, p.z_kind, s); });
+      st = run_named("kan_vocab_ds", s, [&] { return p.few ? launch_few<kGradS>(g, s) : launch_product<T, kGradS>(g, p.z_kind, s); });
       if (st != KAN_OK) return st;
       // dh (+)= dS T: k = rows of the piece
       ProductArgs r = g;
@@ -1065,6 +1267,10 @@ kan_status run_vocab_grad(const VocabArgs& a, hipStream_t s) {
       g.out_dtype = a.dtype;
       g.add = a.accumulate;
       g.factor = x.factor;
+      if (p.few) {
+        if ((st = run_named("kan_vocab_rows", s, [&] { return launch_few_rows(r, s); })) != KAN_OK) return st;
+        r.m = 0;            // (then there are no tiles of it)
+      }
       st = run_named("kan_vocab_grads", s, [&] { return launch_grads<T>(r, g, p.grad_kind, s); });
       if (st != KAN_OK) return st;
     }

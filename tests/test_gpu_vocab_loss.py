@@ -75,6 +75,11 @@ def test_many_tokens(kb, N, V, D, dtype):
     check_all(kb, *draw(N + D, N, V, D, dtype, ("i32", "i64", "u16")[N % 3]), scale=1.0)
 
 
+@pytest.mark.parametrize("N,V,D", [(1, 31, 3), (3, 1000, 70), (31, 33, 129), (32, 2085, 64), (33, 100, 250), (60, 1200001, 12), (63, 4999, 300)])
+def test_few_tokens_in_full_precision(kb, N, V, D):
+    check_all(kb, *draw(N + D, N, V, D, F32, ("i32", "i64")[N % 2]), scale=0.5)
+
+
 @pytest.mark.parametrize("dtype,N,V,D", [(F16, 40, 50001, 1000), (BF16, 2500, 132000, 64), (F32, 300, 150001, 200)])
 def test_tables_in_several_pieces(kb, dtype, N, V, D):
     check_all(kb, *draw(1, N, V, D, dtype), scale=1.0)
