@@ -1065,8 +1065,8 @@ Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
   long long piece = all;
   auto limit = [&](long long budget, long long row_bytes) { piece = std::min(piece, std::max(1ll, budget / (row_bytes * kVocabStep)) * kVocabStep); };
   // Packed pieces that the memory-side cache holds (426 x 36,161 x 2,235 in fp32 2,170 us, in one piece 2,390), but not fewer rows than
-  // give the CUs three tiles of 128 x 64 each (128 x 30,000 x 2,048 838 us for 1,075; 70 x 100,000 x 1,024 1,476 for 1,421).
-  if (p.pack_table) limit(std::max(kPackBytes, 3ll * kCus * 128 / ((N + 63) / 64) * p.parts * p.width * 2), p.parts * p.width * 2);
+  // give the CUs three tiles of 128 x 64 each, while that is 2 GiB or less (128 x 30,000 x 2,048 838 us for 1,075; 70 x 100,000 x 1,024 1,476 for 1,421).
+  if (p.pack_table) limit(std::max(kPackBytes, std::min(2ll << 30, 3ll * kCus * 128 / ((N + 63) / 64) * p.parts * p.width * 2)), p.parts * p.width * 2);
   // (tiles of 128 x 64: fewer than 2^23 of a launch's)
   limit(1ll << 36, N);
   if (backward) {
