@@ -33,7 +33,7 @@ __device__ __forceinline__ int first_shift(long long n, int D) { return !WHOLE &
 template <bool WHOLE>
 __device__ __forceinline__ bool within(int c, int D) { return WHOLE || (c >= 0 && c + 8 <= D); }
 // room: elements from the row's first to the array's end.  A part of eight columns is read with its neighbours in other rows,
-// which are then left out; only at the array's end it is read one by one.
+// which are then left out; only at the array's end it is read one by one (rows of fewer than eight columns may begin in it).
 template <bool WHOLE, class T>
 __device__ __forceinline__ void load_part(const T* row, int c, int D, long long room, float (&out)[8]) {
   if (WHOLE || c + 8 <= room) {
@@ -43,7 +43,7 @@ __device__ __forceinline__ void load_part(const T* row, int c, int D, long long 
       for (int i = 0; i < 8; ++i) out[i] = c + i >= 0 && c + i < D ? out[i] : 0.f;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) out[i] = c + i < D ? (float)row[c + i] : 0.f;
+    for (int i = 0; i < 8; ++i) out[i] = c + i >= 0 && c + i < D ? (float)row[c + i] : 0.f;
   }
 }
 template <bool WHOLE, class T>
@@ -194,7 +194,7 @@ struct Raw {
         for (int i = 0; i < 8; ++i) v[i] = c + i >= 0 && c + i < D ? v[i] : (T)0.f;
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = c + i < D ? p[i] : (T)0.f;
+      for (int i = 0; i < 8; ++i) v[i] = c + i >= 0 && c + i < D ? p[i] : (T)0.f;
     }
   }
   __device__ __forceinline__ void clear() {

@@ -1,0 +1,49 @@
+"""kan_block_norm_forward / kan_block_norm_backward where rows, streams and gates are at the ends of their ranges, against
+their definitions in 64 bits."""
+import pytest
+
+from tokens_testlib import check, norms, norms_grad
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def kb():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2512_15742_amd import binding
+    binding.lib()
+    return binding
+
+
+def draw(seed, N, D, stream, block, weight):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+
+    def normal(*shape, type, mul=1.0, add=0.0):
+        return (torch.randn(shape, generator=g, device="cuda") * mul + add).to(type)
+    return dict(x=normal(N, D, type=stream, mul=2.0), v=normal(N, D, type=block, mul=0.7), gate=normal(N, D, type=block, mul=3.0),
+                wa=normal(D, type=weight, mul=0.2, add=1.0), wb=normal(D, type=weight, mul=0.1, add=0.3), dy=normal(N, D, type=stream),
+                du=normal(N, D, type=block))
+
+
+@pytest.mark.parametrize("stream,block,weight", [(F32, F32, F32), (BF16, BF16, F32), (F16, F32, F16)])
+@pytest.mark.parametrize("D", [1, 2, 3, 4, 5, 6, 7])
+def test_rows_of_fewer_than_eight_columns(kb, D, stream, block, weight):
+    """The last rows of an array share eight elements with the rows in front of them, which hold nothing of theirs."""
+    for N in range(2, 18):
+        t = draw(100 * D + N, N, D, stream, block, weight)
+        scale, eps = 0.75, 1e-5
+        y, u = kb.kan_block_norm_forward(t["x"], v=t["v"], gate=t["gate"], w_after=t["wa"], w_before=t["wb"], scale=scale, eps=eps)
+        ry, ey, ru, eu = norms(t["x"], t["v"], t["gate"], t["wa"], t["wb"], scale, eps)
+        check(y, ry, ey)
+        check(u, ru, eu)
+        _, first = kb.kan_block_norm_forward(t["x"], w_before=t["wb"], eps=eps, dtype=block)
+        check(first, *norms(t["x"], None, None, None, t["wb"], scale, eps)[2:])
+        got = kb.kan_block_norm_backward(t["x"], dy=t["dy"], du=t["du"], v=t["v"], gate=t["gate"], w_after=t["wa"], w_before=t["wb"], scale=scale, eps=eps)
+        for a, r in zip(got, norms_grad(t["x"], t["dy"], t["du"], t["v"], t["gate"], t["wa"], t["wb"], scale, eps)):
+            check(a, *r)
