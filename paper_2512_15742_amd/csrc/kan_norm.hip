@@ -109,12 +109,13 @@ __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf
 // W waves a row, W == 1: four rows a workgroup.
 template <class S, class B, int W, int P, bool WHOLE>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_kernel(const NormArgs a) {
-  __shared__ float sSum[2][W][1];
+  __shared__ float sSum[2][2][W][1];
   const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x;
   const int D = a.D;
   const float inv = 1.f / (float)D;
   const long long rows = (long long)gridDim.x * (W == 1 ? 4 : 1);
-  for (long long n = W == 1 ? (long long)blockIdx.x * 4 + (threadIdx.x >> 6) : (long long)blockIdx.x; n < a.N; n += rows) {
+  int odd = 0;       // (each row has one or two sums: the scratch of a row is another one than that of the row before)
+  for (long long n = W == 1 ? (long long)blockIdx.x * 4 + (threadIdx.x >> 6) : (long long)blockIdx.x; n < a.N; n += rows, odd ^= 1) {
     float x[P][8], v[P][8], g[P][8], w[P][8];
     const int shift = first_shift<WHOLE, 512 * W * P>(n, D);
     const long long room = (a.N - n) * D;
@@ -138,7 +139,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_kernel(const N
       for (int p = 0; p < P; ++p)
   #pragma unroll
         for (int i = 0; i < 8; ++i) ss[0] += v[p][i] * v[p][i];
-      row_sums<W, 1>(ss, sSum[0]);
+      row_sums<W, 1>(ss, sSum[odd][0]);
       const float r = a.scale * rsqrtf(ss[0] * inv + a.eps);
   #pragma unroll
       for (int p = 0; p < P; ++p) {
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void kan_norm_kernel(const N
       for (int p = 0; p < P; ++p)
   #pragma unroll
         for (int i = 0; i < 8; ++i) ss[0] += x[p][i] * x[p][i];
-      row_sums<W, 1>(ss, sSum[1]);
+      row_sums<W, 1>(ss, sSum[odd][1]);
       const float r = rsqrtf(ss[0] * inv + a.eps);
   #pragma unroll
       for (int p = 0; p < P; ++p) {

@@ -47,3 +47,26 @@ def test_rows_of_fewer_than_eight_columns(kb, D, stream, block, weight):
         got = kb.kan_block_norm_backward(t["x"], dy=t["dy"], du=t["du"], v=t["v"], gate=t["gate"], w_after=t["wa"], w_before=t["wb"], scale=scale, eps=eps)
         for a, r in zip(got, norms_grad(t["x"], t["dy"], t["du"], t["v"], t["gate"], t["wa"], t["wb"], scale, eps)):
             check(a, *r)
+
+
+@pytest.mark.parametrize("form", ["first", "last", "both"])
+def test_streams_of_more_rows_than_workgroups(kb, form):
+    """More than 2^20 rows of several waves each: a workgroup takes further rows, with one sum a row or two."""
+    N, D, part = 2 ** 20 + 3 * 2 ** 15 + 77, 1032, 2 ** 15
+    g = torch.Generator(device="cuda").manual_seed(31)
+    x = torch.empty((N, D), dtype=BF16, device="cuda")
+    for n in range(0, N, part):
+        x[n:n + part] = torch.randn((min(part, N - n), D), generator=g, device="cuda") * (0.25 + torch.rand((min(part, N - n), 1), generator=g, device="cuda"))
+    v = None if form == "first" else x.flip(0)
+    wb = (torch.randn(D, generator=g, device="cuda") * 0.1 + 0.3) if form != "last" else None
+    args = dict(v=v, w_before=wb, scale=0.5, eps=1e-5, want_u=form != "last")
+    y, u = kb.kan_block_norm_forward(x, **args)
+    for n in [*range(0, N - 2 ** 20, part // 4), 2 ** 19, *range(2 ** 20 - part // 4, N, part // 4)]:      # rows of workgroups with two of them, and others
+        rows = slice(n, min(N, n + part // 4))
+        ry, ey, ru, eu = norms(x[rows], None if v is None else v[rows], None, None, wb, 0.5, 1e-5)
+        if y is not None:
+            check(y[rows], ry, ey)
+        if u is not None:
+            check(u[rows], ru, eu)
+    again = kb.kan_block_norm_forward(x, **args)
+    assert all(a is None or torch.equal(a, b) for a, b in zip((y, u), again))
