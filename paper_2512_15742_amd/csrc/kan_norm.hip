@@ -5,7 +5,7 @@
 //
 // Backward, from y, v, gate and the gradients dy, du (t = du w_before, m = v rv, s = sigma(gate)):
 //   gy = dy + ry (t - y ry mean(t y ry))                       = dx, the gradient of the stream in front of the block
-//   q  = scale s gy w_after,   dv = rv (q - m mean(q m)),   dgate = scale gy w_after m s (1 - s)
+//   q  = scale s gy w_after,   dv = rv (q - m mean(q m)),   dgate = scale gy w_after m sigma(gate) sigma(-gate)
 //   dw_before = sum du y ry,   dw_after = sum scale s gy m     (over the tokens)
 //
 // Bound by the bytes of the rows: each is read once, a row stays in the registers of one to sixteen waves, eight columns a
@@ -105,6 +105,12 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float (*scratch)[K]) {
 }
 
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+// sigma(z) and its derivative sigma(z) sigma(-z): both from e^-|z|, so that nothing cancels (1 - sigma(z) is 0 from z = 17 on).
+__device__ __forceinline__ void sigmoid_and_slope(float z, float& s, float& slope) {
+  const float e = __expf(-fabsf(z)), r = __builtin_amdgcn_rcpf(1.f + e);
+  s = z < 0.f ? e * r : r;
+  slope = e * r * r;
+}
 
 // W waves a row, W == 1: four rows a workgroup.
 template <class S, class B, int W, int P, bool WHOLE>
@@ -281,9 +287,11 @@ __global__ __launch_bounds__(64 * W, P == 1 && WHOLE ? 4 : (W == 16 ? 4 : 2)) vo
         float dg[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float s = a.gate ? sigmoid(r.g[p][i]) : 1.f, m = r.v[p][i] * rv, e = a.scale * q[p][i];
+          float s = 1.f, slope = 0.f;
+          if (a.gate) sigmoid_and_slope(r.g[p][i], s, slope);
+          const float m = r.v[p][i] * rv, e = a.scale * q[p][i];
           sum2[p][i] += s * e * m;
-          dg[i] = e * (w2[p][i] * m) * (s * (1.f - s));
+          dg[i] = e * (w2[p][i] * m) * slope;
           q[p][i] = s * e * w2[p][i];
           sq[0] += q[p][i] * m;
         }

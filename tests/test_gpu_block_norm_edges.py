@@ -70,3 +70,18 @@ def test_streams_of_more_rows_than_workgroups(kb, form):
             check(u[rows], ru, eu)
     again = kb.kan_block_norm_forward(x, **args)
     assert all(a is None or torch.equal(a, b) for a, b in zip((y, u), again))
+
+
+def test_gradient_of_gates_far_from_zero(kb):
+    """dgate goes with sigma(z) sigma(-z): as exact for open gates, where 1 - sigma is a difference of nearly equal numbers, as for
+    closed ones.  Its bound is norms_grad's (a quotient of the exponential is off by up to |z| half steps, the sums by 128), in terms of
+    the whole product."""
+    N, D = 22, 96
+    t = draw(41, N, D, F32, F32, F32)
+    z = torch.tensor([5.0, 8, 10, 12, 14, 16, 17, 18, 20, 25, 30], device="cuda")
+    t["gate"] = (torch.cat([z, -z])[:, None] + torch.linspace(0, 0.5, D, device="cuda")).contiguous()
+    got = kb.kan_block_norm_backward(t["x"], dy=t["dy"], du=t["du"], v=t["v"], gate=t["gate"], w_after=t["wa"], w_before=t["wb"], scale=0.5)
+    ref, bound = norms_grad(t["x"], t["dy"], t["du"], t["v"], t["gate"], t["wa"], t["wb"], 0.5, 1e-6)[2]
+    zd = t["gate"].double()
+    other = torch.sigmoid(-zd)
+    check(got[2], ref / (1 - torch.sigmoid(zd)) * other, bound * other)
