@@ -348,12 +348,12 @@ __device__ __forceinline__ void product(const ProductArgs& g, const unsigned blo
     // In units of log 2: the exponentials are the hardware's, of base 2.
     float2* const sStat = (float2*)sRing;         // [WM][BN]
     const float scale = g.scale * 1.44269504088896f;
-    const int first_row = g.v0 + m0 + wm;
+    const int here = g.V - g.v0 - m0 - wm;       // rows of the table from the wave's first on (differences: v0 + m0 + wm may pass 2^31)
 #pragma unroll
     for (int j = 0; j < CB; ++j) {
-      int rows = g.V - (first_row + 4 * lh);
+      int rows = here - 4 * lh;
       asm volatile("" : "+v"(rows));       // (compared anew: 64 masks kept for all j would not fit the scalar registers)
-      const bool whole = first_row + 32 * RB <= g.V;
+      const bool whole = here >= 32 * RB;
       float z[RB][16], top = -INFINITY, sum = 0.f;
 #pragma unroll
       for (int i = 0; i < RB; ++i)
@@ -403,11 +403,11 @@ __device__ __forceinline__ void product(const ProductArgs& g, const unsigned blo
       if constexpr (EPI == kGradS) {
         const int n = min(nb + ln, n_here - 1);
         const float lse = g.lse[n] * 1.44269504088896f, weight = g.weight[n], scale = g.scale * 1.44269504088896f;
-        const int m_first = g.v0 + m0 + wm + 4 * lh;
-        int rows = g.V - m_first, hit = g.targets[n] - m_first;
+        const int here = g.V - g.v0 - m0 - wm;
+        int rows = here - 4 * lh, hit = (int)((uint32_t)g.targets[n] - (uint32_t)(g.v0 + m0) - (uint32_t)(wm + 4 * lh));
         asm volatile("" : "+v"(rows), "+v"(hit));
         // (a target, or the table's end, among the wave's rows)
-        const bool special = __any((unsigned)hit < 32u * RB) || g.v0 + m0 + wm + 32 * RB > g.V;
+        const bool special = __any((unsigned)hit < 32u * RB) || here < 32 * RB;
 #pragma unroll
         for (int i = 0; i < RB; ++i)
 #pragma unroll
@@ -577,7 +577,7 @@ __global__ __launch_bounds__(kThreads) void kan_vocab_few_kernel(const ProductAr
     } else {
       if (n < n_here) {
         const float lse = g.lse[n] * 1.44269504088896f, weight = g.weight[n];
-        const int hit = g.targets[n] - g.v0 - m0 - m;
+        const int hit = (int)((uint32_t)g.targets[n] - (uint32_t)(g.v0 + m0) - (uint32_t)m);
         float v[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -1067,8 +1067,9 @@ Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
   // Packed pieces that the memory-side cache holds (426 x 36,161 x 2,235 in fp32 2,170 us, in one piece 2,390), but not fewer rows than
   // give the CUs three tiles of 128 x 64 each, while that is 2 GiB or less (128 x 30,000 x 2,048 838 us for 1,075; 70 x 100,000 x 1,024 1,476 for 1,421).
   if (p.pack_table) limit(std::max(kPackBytes, std::min(2ll << 30, 3ll * kCus * 128 / ((N + 63) / 64) * p.parts * p.width * 2)), p.parts * p.width * 2);
-  // (tiles of 128 x 64: fewer than 2^23 of a launch's)
+  // (fewer than 2^24 workgroups a launch, whose threads have 32 bits: tiles of 128 x 64, few: 32 rows)
   limit(1ll << 36, N);
+  limit(p.few ? 1ll << 28 : 1ll << 30, 1);
   if (backward) {
     limit(kPieceBytes, p.parts * N * 2);
     limit(1ll << 35, D);
@@ -1163,7 +1164,8 @@ kan_status run_vocab_loss(const VocabArgs& a, hipStream_t s) {
     g.stats = (float2*)(ws + p.stats);
     kan_status st;
     g.b = p.pack_rows ? Operand{ws + p.h, p.width, a.N * p.width, (int)a.N, (int)p.width} : Operand{a.h, a.D, 0, (int)a.N, a.D};
-    for (int v0 = 0, i = 0; i < p.pieces; ++i, v0 += p.piece) {
+    for (int i = 0; i < p.pieces; ++i) {
+      const int v0 = i * p.piece;
       PackArgs job;
       g.v0 = v0;
       g.m = std::min(p.piece, a.V - v0);
@@ -1177,7 +1179,7 @@ kan_status run_vocab_loss(const VocabArgs& a, hipStream_t s) {
     }
     return run_named("kan_vocab_join", s, [&] {
       const int rows = p.stat_rows;
-      const JoinArgs j = {g.stats, a.h, a.table, a.targets, a.loss, a.lse, (a.V + rows - 1) / rows, (int)a.N, a.D, a.id_dtype, (uint32_t)a.V, a.scale};
+      const JoinArgs j = {g.stats, a.h, a.table, a.targets, a.loss, a.lse, (a.V - 1) / rows + 1, (int)a.N, a.D, a.id_dtype, (uint32_t)a.V, a.scale};
       return with_float(a.dtype, [&](auto i) {
         if (a.N <= 1024) hipLaunchKernelGGL((kan_vocab_join_kernel<decltype(i), 1>), dim3((unsigned)a.N), dim3(256), 0, s, j);
         else hipLaunchKernelGGL((kan_vocab_join_kernel<decltype(i), 16>), dim3((unsigned)((a.N + 15) / 16)), dim3(256), 0, s, j);
@@ -1208,8 +1210,8 @@ kan_status run_vocab_grad(const VocabArgs& a, hipStream_t s) {
   return with_operand(a.dtype, [&](auto t) -> kan_status {
     typedef decltype(t) T;
     const Operand h = {ws + p.h, p.width, a.N * p.width, N, (int)p.width};
-    for (int v0 = 0, i = 0; i < p.pieces; ++i, v0 += p.piece) {
-      const int rows = std::min(p.piece, a.V - v0);
+    for (int i = 0; i < p.pieces; ++i) {
+      const int v0 = i * p.piece, rows = std::min(p.piece, a.V - v0);
       const long long ds_part = a.N * (long long)p.piece;
       PackArgs job;
       const Operand table = table_rows(a, p, ws, v0, rows, &job);
