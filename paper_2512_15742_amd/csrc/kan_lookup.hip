@@ -59,8 +59,9 @@ __global__ __launch_bounds__(kThreads) void kan_lookup_kernel(const T* __restric
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (n[u] >= N) continue;
+      const float by = id[u] < V ? scale : 0.f;        // (0 * infinity would be no zero)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[u][i] *= scale;
+      for (int i = 0; i < 8; ++i) v[u][i] *= by;
       store_cols(y + n[u] * D, c[u], D, v[u]);
     }
   }
