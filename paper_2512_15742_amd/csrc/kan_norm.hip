@@ -107,9 +107,9 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float (*scratch)[K]) {
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 // sigma(z) and its derivative sigma(z) sigma(-z): both from e^-|z|, so that nothing cancels (1 - sigma(z) is 0 from z = 17 on).
 __device__ __forceinline__ void sigmoid_and_slope(float z, float& s, float& slope) {
-  const float e = __expf(-fabsf(z)), r = __builtin_amdgcn_rcpf(1.f + e);
-  s = z < 0.f ? e * r : r;
-  slope = e * r * r;
+  const float e = __expf(-fabsf(z)), r = __builtin_amdgcn_rcpf(1.f + e), least = e * r;       // least: the smaller of sigma(z), sigma(-z)
+  s = z < 0.f ? least : r;
+  slope = fmaf(-least, least, least);
 }
 
 // W waves a row, W == 1: four rows a workgroup.
