@@ -327,6 +327,16 @@ __global__ __launch_bounds__(64 * W, P == 1 && WHOLE ? 4 : (W == 16 ? 4 : 2)) vo
   }
 }
 
+// Sum in a tree: log2(K) roundings one behind the other in place of K.
+template <int K>
+__device__ __forceinline__ float tree_sum(float (&v)[K]) {
+#pragma unroll
+  for (int d = K / 2; d >= 1; d /= 2)
+#pragma unroll
+    for (int k = 0; k < d; ++k) v[k] += v[k + d];
+  return v[0];
+}
+
 // 16 columns a workgroup, 64 shares of the groups.
 __global__ __launch_bounds__(kReduceThreads) void kan_norm_reduce_kernel(const float* __restrict__ partial, int groups, int D, void* first, void* second,
                                                                          int dtype) {
@@ -339,16 +349,16 @@ __global__ __launch_bounds__(kReduceThreads) void kan_norm_reduce_kernel(const f
       float v[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) v[u] = r + u * 64 < groups ? src[(long long)(r + u * 64) * D + c] : 0.f;
-#pragma unroll
-      for (int u = 0; u < 8; ++u) s += v[u];
+      s += tree_sum(v);
     }
   }
   sSum[share][lane] = s;
   __syncthreads();
   if (share == 0 && c < D) {
-    s = 0.f;
+    float v[64];
 #pragma unroll
-    for (int k = 0; k < 64; ++k) s += sSum[k][lane];
+    for (int k = 0; k < 64; ++k) v[k] = sSum[k][lane];
+    s = tree_sum(v);
     void* const out = blockIdx.y == 0 ? first : second;
     if (dtype == KAN_F32) ((float*)out)[c] = s;
     else if (dtype == KAN_F16) ((f16*)out)[c] = (f16)s;

@@ -85,3 +85,15 @@ def test_gradient_of_gates_far_from_zero(kb):
     zd = t["gate"].double()
     other = torch.sigmoid(-zd)
     check(got[2], ref / (1 - torch.sigmoid(zd)) * other, bound * other)
+
+
+def test_sums_of_the_groups_are_trees(kb):
+    """Rows of ones: a term of dw_before is an entry of du, exact, and only its sum over 512 rows, one a group, is rounded.  A
+    rounding is off by at most U of its value, evenly: a level of a tree with n sums of S / n adds S^2 U^2 / (3 n) to the mean square,
+    all levels 2/3 S^2 U^2 at most (64 sums one behind the other: up to 64/9 S^2 U^2)."""
+    N, D = 512, 2048
+    y = torch.ones((N, D), device="cuda")
+    du = torch.rand((N, D), generator=torch.Generator(device="cuda").manual_seed(51), device="cuda") + 1.0
+    got = kb.kan_block_norm_backward(y, du=du, w_before=torch.ones(D, device="cuda"), eps=1e-12)[3]
+    ref = du.double().sum(0)
+    assert float(((got.double() - ref) / ref).square().mean().sqrt()) <= (2 / 3) ** 0.5 * 2.0 ** -24
