@@ -6,7 +6,7 @@
 //
 // Forward: tiles of z stay in registers; each leaves the maximum and the sum of exponentials of its part of a row, which a
 // small launch joins.  Backward: piece by piece of the table (z formed once more: dS of 8,192 x 131,072 tokens and rows would
-// be 2.1 GB, pieces of 256 MiB take 1.5 % longer than all of it), dS of the piece in the workspace, and two products with it.
+// be 2.1 GB, pieces of 256 MiB, of each part, take 1.5 % longer than all of it), dS of the piece in the workspace, and two products with it.
 // All products run on the matrix cores with fp32 sums.
 //
 // Operands are 16-bit numbers.  fp32 rows travel as three bf16 parts (24 bits together; of the nine products of parts the three
@@ -18,7 +18,7 @@
 // Bound: few tokens by the bytes of the table (one token x 65,536 x 2,048 in bf16 51 us, 5.3 TB/s); many by the matrix cores and
 // the power that they draw (8,192 x 131,072 x 2,048: the loss 3.6 ms, 1.21 PFLOP/s; loss and gradients 15.0 ms, 1.17 PFLOP/s over
 // four products; the clock falls to 1.7 GHz, matrix units busy 62 % of it in the loss, 50 % with dS, 69 % in the
-// gradients).  Between, launches and tiles that do not fill the CUs (500 x 10,007 x 256 in fp32 123 us in seven launches).
+// gradients).  Between, launches and tiles that do not fill the CUs (500 x 10,007 x 256 in fp32 114 us in seven launches).
 #include <float.h>
 
 #include <algorithm>
@@ -111,7 +111,7 @@ __device__ __forceinline__ void copies_done() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
 }
 
-// Which parts of A and B the six products of three parts each take, the smallest first: two bits a product.
+// Which parts of A and B the six products of three parts each take (dT of fp32 rows), the smallest first: two bits a product.
 constexpr uint32_t kPartA = 2u | 1u << 2 | 0u << 4 | 1u << 6 | 0u << 8 | 0u << 10;
 constexpr uint32_t kPartB = 0u | 1u << 2 | 2u << 4 | 0u << 6 | 1u << 8 | 0u << 10;
 
@@ -218,132 +218,27 @@ struct Shape {
   static constexpr int BM = 32 * RB * WM, BN = 32 * CB * WN, kLds = kSlots * (BM + BN) * kStep * 2;
 };
 
-template <class T, bool AK, bool BK, int EPI, class S>
-__device__ __forceinline__ void product(const ProductArgs& g, const unsigned block, unsigned char* const sRing) {
-  constexpr int RB = S::RB, CB = S::CB, WM = S::WM, WN = S::WN, kSlots = S::kSlots, BM = S::BM, BN = S::BN;
-  typedef Tile<T, AK, BM> TA;
-  typedef Tile<T, BK, BN> TB;
-  constexpr int kSlot = TA::kBytes + TB::kBytes, kCopies = TA::kCopies + TB::kCopies;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int ln = lane & 31, lh = lane >> 5;
+// Which tile, and which share of the contraction, a workgroup has: runs of consecutive work items per XCD; eight tiles of n by as many
+// of m as it has workgroups.
+__device__ __forceinline__ bool place(unsigned block, unsigned nmt, unsigned nnt, unsigned splits, int* mt, int* nt, int* split) {
+  const unsigned tiles = nmt * nnt, W = tiles * splits, L = block, xcd = L & 7u, q = W >> 3, r = W & 7u;
+  if (L >= W) return false;
+  const unsigned work = xcd * q + min(xcd, r) + (L >> 3), item = work % tiles;
+  *split = (int)(work / tiles);
+  const unsigned group = item / (8 * nmt), first = group * 8, width = min(8u, nnt - first), in = item - first * nmt;
+  *mt = (int)(in / width);
+  *nt = (int)(first + in % width);
+  return true;
+}
+
+// What becomes of a tile's sums, acc[i][j][r]: m = m0 + wm + 32 i + 8 (r / 4) + 4 lh + r % 4, n = n0 + wn + 32 j + ln.  All waves are done with
+// the LDS.
+template <class T, int EPI, class S>
+__device__ __forceinline__ void finish(const ProductArgs& g, f32x16 (&acc)[S::RB][S::CB], const int m0, const int n0, const int split, const int n_here,
+                                       unsigned char* const sRing) {
+  constexpr int RB = S::RB, CB = S::CB, WM = S::WM, BM = S::BM, BN = S::BN;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, lh = lane >> 5;
   const int wm = (wave % WM) * 32 * RB, wn = (wave / WM) * 32 * CB;
-  const int n_here = EPI != kGradTable && g.count ? min(g.n, *g.count) : g.n, k_here = EPI == kGradTable && g.count ? min(g.k, *g.count) : g.k;
-  // Runs of consecutive work items per XCD; eight tiles of n by as many of m as it has workgroups.
-  int mt, nt, split;
-  const unsigned nmt = (unsigned)(g.m + BM - 1) / BM, nnt = (unsigned)(n_here + BN - 1) / BN, tiles = nmt * nnt, W = tiles * (unsigned)g.splits;
-  {
-    const unsigned L = block, xcd = L & 7u, q = W >> 3, r = W & 7u;
-    if (L >= W) return;
-    const unsigned work = xcd * q + min(xcd, r) + (L >> 3), item = work % tiles;
-    split = (int)(work / tiles);
-    const unsigned group = item / (8 * nmt), first = group * 8, width = min(8u, nnt - first), in = item - first * nmt;
-    mt = (int)(in / width);
-    nt = (int)(first + in % width);
-  }
-  const int m0 = mt * BM, n0 = nt * BN;
-  TA A;
-  TB B;
-  A.init(g.a, m0, wave, lane, wm);
-  B.init(g.b, n0, wave, lane, wn);
-  const int depth_a = min(g.a.depth, AK ? g.a.depth : k_here), depth_b = min(g.b.depth, BK ? g.b.depth : k_here);
-  const int ksteps = (k_here + kStep - 1) / kStep, all = g.parts == 1 ? ksteps : 6 * ksteps;
-  const int s0 = (int)((long long)all * split / g.splits), total = (int)((long long)all * (split + 1) / g.splits) - s0;
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sRing;
-
-  // The next copies: product of parts, k, slot.  Past the last one everything is behind the buffers' ends.
-  // With one tile of n every row of the table is read by one workgroup: each begins at another k, since rows of 2^n bytes in step
-  // would meet in the same memory channels.
-  const int turn = EPI != kGradRows && nnt == 1 && g.parts == 1 && ksteps > 1 ? (int)((unsigned)mt * 5u % (unsigned)ksteps) : 0;
-  int cq = g.parts == 1 ? 0 : s0 / max(ksteps, 1), ck = (s0 - cq * ksteps + turn) * kStep, cs = 0, left = total;
-  u32x4 ra, rb;
-  A.aim(g.parts == 1 ? 0u : kPartA >> (2 * cq) & 3u, depth_a, ck);
-  B.aim(g.parts == 1 ? 0u : kPartB >> (2 * cq) & 3u, depth_b, ck);
-  ra = A.buffer();
-  rb = B.buffer();
-  auto copy = [&](int j) __attribute__((always_inline)) {
-    if (j < TA::kCopies) A.copy(ra, j, wave, lds0 + (uint32_t)(cs * kSlot), ck, depth_a);
-    else B.copy(rb, j - TA::kCopies, wave, lds0 + (uint32_t)(cs * kSlot + TA::kBytes), ck, depth_b);
-  };
-  auto next = [&]() __attribute__((always_inline)) {
-    cs = cs + 1 == kSlots ? 0 : cs + 1;
-    ck += kStep;
-    A.move();
-    B.move();
-    if (--left <= 0) {
-      A.deep = B.deep = 0;
-    } else if (ck >= k_here) {
-      ck = 0;
-      cq += g.parts > 1 ? 1 : 0;
-      A.aim(g.parts == 1 ? 0u : kPartA >> (2 * cq) & 3u, depth_a, 0);
-      B.aim(g.parts == 1 ? 0u : kPartB >> (2 * cq) & 3u, depth_b, 0);
-    }
-    ra = A.buffer();
-    rb = B.buffer();
-  };
-  f32x16 acc[RB][CB];
-#pragma unroll
-  for (int i = 0; i < RB; ++i)
-#pragma unroll
-    for (int j = 0; j < CB; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-#pragma unroll
-  for (int s = 0; s < kSlots; ++s) {
-#pragma unroll
-    for (int j = 0; j < kCopies; ++j) copy(j);
-    next();
-  }
-  struct Frags {
-    uint4 a[2][RB], b[2][CB];
-  };
-  Frags f[2];
-  constexpr int kReadsA = 2 * RB * TA::kReads, kReadsAll = kReadsA + 2 * CB * TB::kReads;
-  auto read = [&](const unsigned char* slot, int i, Frags& to) __attribute__((always_inline)) {
-    if (i < kReadsA) {
-      const int j = i % TA::kReads, b = i / TA::kReads % RB, h = i / TA::kReads / RB;
-      A.fragment(slot, b, h, j, to.a[h][b]);
-    } else {
-      i -= kReadsA;
-      const int j = i % TB::kReads, b = i / TB::kReads % CB, h = i / TB::kReads / CB;
-      B.fragment(slot + TA::kBytes, b, h, j, to.b[h][b]);
-    }
-  };
-  copies_done<(kSlots - 1) * kCopies>();
-  __builtin_amdgcn_s_barrier();
-#pragma unroll
-  for (int i = 0; i < kReadsAll; ++i) read(sRing, i, f[0]);
-
-  int rs = 0;
-  auto step = [&](auto P) __attribute__((always_inline)) {
-    constexpr int p = decltype(P)::value, kMfmas = 2 * RB * CB, kSpread = kMfmas > 4 ? kMfmas - 2 : kMfmas;
-    copies_done<(kSlots - 2) * kCopies>();
-    __builtin_amdgcn_s_barrier();
-    rs = rs + 1 == kSlots ? 0 : rs + 1;
-    const unsigned char* const slot = sRing + rs * kSlot;
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < kMfmas; ++i) {
-      const int h = i / (RB * CB), a = i / CB % RB, b = i % CB;
-      acc[a][b] = mfma<T>(f[p].a[h][a], f[p].b[h][b], acc[a][b]);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int u = i * kReadsAll / kSpread; u < (i + 1) * kReadsAll / kSpread && u < kReadsAll; ++u) read(slot, u, f[p ^ 1]);
-#pragma unroll
-      for (int u = i * kCopies / kMfmas; u < (i + 1) * kCopies / kMfmas; ++u) copy(u);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    next();
-  };
-  int s = 0;
-  for (; s + 2 <= total; s += 2) {
-    step(std::integral_constant<int, 0>{});
-    step(std::integral_constant<int, 1>{});
-  }
-  if (s < total) step(std::integral_constant<int, 0>{});
-  copies_done<0>();
-  __syncthreads();
-
-  // acc[i][j][r]: m = wm + 32 i + 8 (r / 4) + 4 lh + r % 4, n = wn + 32 j + ln
   if constexpr (EPI == kStats) {
     // In units of log 2: the exponentials are the hardware's, of base 2.
     float2* const sStat = (float2*)sRing;         // [WM][BN]
@@ -451,6 +346,124 @@ __device__ __forceinline__ void product(const ProductArgs& g, const unsigned blo
   }
 }
 
+template <class T, bool AK, bool BK, int EPI, class S>
+__device__ __forceinline__ void product(const ProductArgs& g, const unsigned block, unsigned char* const sRing) {
+  constexpr int RB = S::RB, CB = S::CB, WM = S::WM, WN = S::WN, kSlots = S::kSlots, BM = S::BM, BN = S::BN;
+  typedef Tile<T, AK, BM> TA;
+  typedef Tile<T, BK, BN> TB;
+  constexpr int kSlot = TA::kBytes + TB::kBytes, kCopies = TA::kCopies + TB::kCopies;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = (wave % WM) * 32 * RB, wn = (wave / WM) * 32 * CB;
+  const int n_here = EPI != kGradTable && g.count ? min(g.n, *g.count) : g.n, k_here = EPI == kGradTable && g.count ? min(g.k, *g.count) : g.k;
+  int mt, nt, split;
+  const unsigned nnt = (unsigned)(n_here + BN - 1) / BN;
+  if (!place(block, (unsigned)(g.m + BM - 1) / BM, nnt, (unsigned)g.splits, &mt, &nt, &split)) return;
+  const int m0 = mt * BM, n0 = nt * BN;
+  TA A;
+  TB B;
+  A.init(g.a, m0, wave, lane, wm);
+  B.init(g.b, n0, wave, lane, wn);
+  const int depth_a = min(g.a.depth, AK ? g.a.depth : k_here), depth_b = min(g.b.depth, BK ? g.b.depth : k_here);
+  const int ksteps = (k_here + kStep - 1) / kStep, all = g.parts == 1 ? ksteps : 6 * ksteps;
+  const int s0 = (int)((long long)all * split / g.splits), total = (int)((long long)all * (split + 1) / g.splits) - s0;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sRing;
+
+  // The next copies: product of parts, k, slot.  Past the last one everything is behind the buffers' ends.
+  // With one tile of n every row of the table is read by one workgroup: each begins at another k, since rows of 2^n bytes in step
+  // would meet in the same memory channels.
+  const int turn = EPI != kGradRows && nnt == 1 && g.parts == 1 && ksteps > 1 ? (int)((unsigned)mt * 5u % (unsigned)ksteps) : 0;
+  int cq = g.parts == 1 ? 0 : s0 / max(ksteps, 1), ck = (s0 - cq * ksteps + turn) * kStep, cs = 0, left = total;
+  u32x4 ra, rb;
+  A.aim(g.parts == 1 ? 0u : kPartA >> (2 * cq) & 3u, depth_a, ck);
+  B.aim(g.parts == 1 ? 0u : kPartB >> (2 * cq) & 3u, depth_b, ck);
+  ra = A.buffer();
+  rb = B.buffer();
+  auto copy = [&](int j) __attribute__((always_inline)) {
+    if (j < TA::kCopies) A.copy(ra, j, wave, lds0 + (uint32_t)(cs * kSlot), ck, depth_a);
+    else B.copy(rb, j - TA::kCopies, wave, lds0 + (uint32_t)(cs * kSlot + TA::kBytes), ck, depth_b);
+  };
+  auto next = [&]() __attribute__((always_inline)) {
+    cs = cs + 1 == kSlots ? 0 : cs + 1;
+    ck += kStep;
+    A.move();
+    B.move();
+    if (--left <= 0) {
+      A.deep = B.deep = 0;
+    } else if (ck >= k_here) {
+      ck = 0;
+      cq += g.parts > 1 ? 1 : 0;
+      A.aim(g.parts == 1 ? 0u : kPartA >> (2 * cq) & 3u, depth_a, 0);
+      B.aim(g.parts == 1 ? 0u : kPartB >> (2 * cq) & 3u, depth_b, 0);
+    }
+    ra = A.buffer();
+    rb = B.buffer();
+  };
+  f32x16 acc[RB][CB];
+#pragma unroll
+  for (int i = 0; i < RB; ++i)
+#pragma unroll
+    for (int j = 0; j < CB; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+#pragma unroll
+  for (int s = 0; s < kSlots; ++s) {
+#pragma unroll
+    for (int j = 0; j < kCopies; ++j) copy(j);
+    next();
+  }
+  struct Frags {
+    uint4 a[2][RB], b[2][CB];
+  };
+  Frags f[2];
+  constexpr int kReadsA = 2 * RB * TA::kReads, kReadsAll = kReadsA + 2 * CB * TB::kReads;
+  auto read = [&](const unsigned char* slot, int i, Frags& to) __attribute__((always_inline)) {
+    if (i < kReadsA) {
+      const int j = i % TA::kReads, b = i / TA::kReads % RB, h = i / TA::kReads / RB;
+      A.fragment(slot, b, h, j, to.a[h][b]);
+    } else {
+      i -= kReadsA;
+      const int j = i % TB::kReads, b = i / TB::kReads % CB, h = i / TB::kReads / CB;
+      B.fragment(slot + TA::kBytes, b, h, j, to.b[h][b]);
+    }
+  };
+  copies_done<(kSlots - 1) * kCopies>();
+  __builtin_amdgcn_s_barrier();
+#pragma unroll
+  for (int i = 0; i < kReadsAll; ++i) read(sRing, i, f[0]);
+
+  int rs = 0;
+  auto step = [&](auto P) __attribute__((always_inline)) {
+    constexpr int p = decltype(P)::value, kMfmas = 2 * RB * CB, kSpread = kMfmas > 4 ? kMfmas - 2 : kMfmas;
+    copies_done<(kSlots - 2) * kCopies>();
+    __builtin_amdgcn_s_barrier();
+    rs = rs + 1 == kSlots ? 0 : rs + 1;
+    const unsigned char* const slot = sRing + rs * kSlot;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < kMfmas; ++i) {
+      const int h = i / (RB * CB), a = i / CB % RB, b = i % CB;
+      acc[a][b] = mfma<T>(f[p].a[h][a], f[p].b[h][b], acc[a][b]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = i * kReadsAll / kSpread; u < (i + 1) * kReadsAll / kSpread && u < kReadsAll; ++u) read(slot, u, f[p ^ 1]);
+#pragma unroll
+      for (int u = i * kCopies / kMfmas; u < (i + 1) * kCopies / kMfmas; ++u) copy(u);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    next();
+  };
+  int s = 0;
+  for (; s + 2 <= total; s += 2) {
+    step(std::integral_constant<int, 0>{});
+    step(std::integral_constant<int, 1>{});
+  }
+  if (s < total) step(std::integral_constant<int, 0>{});
+  copies_done<0>();
+  __syncthreads();
+
+  finish<T, EPI, S>(g, acc, m0, n0, split, n_here, sRing);
+}
+
 constexpr int waves_of(int lds) { return lds <= 81920 ? 2 : 1; }      // workgroups of four waves that a CU is to hold
 template <class T, bool AK, bool BK, int EPI, class S>
 __global__ __launch_bounds__(kThreads, waves_of(S::kLds)) void kan_vocab_product_kernel(const ProductArgs g) {
@@ -465,64 +478,61 @@ __global__ __launch_bounds__(kThreads, waves_of(S::kLds)) void kan_vocab_grads_k
   else product<T, false, false, kGradTable, S>(table, blockIdx.x - row_blocks, sRing);
 }
 
-// ---- few tokens, fp32 -------------------------------------------------------------------------------------------------
-// The table is read as it is, three times for loss and gradients, and split into its parts in registers; the parts in the
-// workspace are one and a half times its bytes, written twice and read three times, by tiles whose steps are six times as many.
-// NB blocks of 32 tokens; the product of the first parts and the smaller ones have sums of their own.  Bound by the reads of the
-// table, from two blocks on by those of the tokens' parts out of L2.  Loss and gradients, with parts in the workspace and so (us):
-// 6 x 83,911 x 2,952 3,308 and 1,028 (z 3.4 to 4.3 TB/s), 18 x 81,628 x 128 173 and 93, 20 x 2,000 x 256 50 and 38,
-// 38 x 9,283 x 1,984 300 and 194, 64 x 30,000 x 1,024 329 and 293; four blocks: 65 x 30,000 x 1,024 386 and 402.
-template <int NB>
+// ---- fp32: products with the table ------------------------------------------------------------------------------------
+// z and dh read the table as it is and split it into its parts in registers.  (Parts in the workspace are one and a half times its bytes, written twice
+// and read three times, by tiles whose steps are six times as many: loss and gradients of 65 x 100,000 x 2,048 so 2,916 us, of 128 x 30,000 x 2,048 824, of
+// 500 x 1,300 x 4,000 397; now 1,148, 420 and 203.)  The product of the first parts and the smaller ones have sums of their own.  Bound by the
+// reads of the table up to about 64 tokens (64 x 30,000 x 1,024: 42 us for the loss, 176 with gradients), by the matrix cores beyond (1,024 x 30,000 x
+// 2,048: the loss 633 us, 1.19 PFLOP/s of the parts).
+
+// The next bf16 part of two numbers, and what is left of them.
+__device__ __forceinline__ uint32_t next_part(float& x, float& y, bool last = false) {
+  typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 t = {(bf16)x, (bf16)y};
+  const uint32_t both = __builtin_bit_cast(uint32_t, t);
+  if (!last) {
+    x -= __builtin_bit_cast(float, both << 16);
+    y -= __builtin_bit_cast(float, both & 0xffff0000u);
+  }
+  return both;
+}
+
 struct FewSums {
-  f32x16 high[NB], low[NB];
+  f32x16 high, low;
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int j = 0; j < NB; ++j)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) high[j][i] = low[j][i] = 0.f;
+    for (int i = 0; i < 16; ++i) high[i] = low[i] = 0.f;
   }
-  // v: eight k of a row of A; b: rows of B, their parts `part` further
-  __device__ __forceinline__ void add(float (&v)[8], const bf16* const (&b)[NB], long long k, long long part) {
+  // v: eight k of a row of A; b: a row of B, its parts `part` further
+  __device__ __forceinline__ void add(float (&v)[8], const bf16* b, long long part) {
     uint4 a[3];
 #pragma unroll
-    for (int p = 0; p < 3; ++p) {
-      bf16x8 t;
+    for (int p = 0; p < 3; ++p) a[p] = make_uint4(next_part(v[0], v[1]), next_part(v[2], v[3]), next_part(v[4], v[5]), next_part(v[6], v[7]));
+    uint4 w[3];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        t[i] = (bf16)v[i];
-        v[i] -= (float)t[i];
-      }
-      a[p] = __builtin_bit_cast(uint4, t);
-    }
-#pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      uint4 w[3];
-#pragma unroll
-      for (int p = 0; p < 3; ++p) w[p] = *(const uint4*)(b[j] + p * part + k);
-      low[j] = mfma<bf16>(a[2], w[0], low[j]);
-      low[j] = mfma<bf16>(a[1], w[1], low[j]);
-      low[j] = mfma<bf16>(a[0], w[2], low[j]);
-      low[j] = mfma<bf16>(a[1], w[0], low[j]);
-      low[j] = mfma<bf16>(a[0], w[1], low[j]);
-      high[j] = mfma<bf16>(a[0], w[0], high[j]);
-    }
+    for (int p = 0; p < 3; ++p) w[p] = *(const uint4*)(b + p * part);
+    low = mfma<bf16>(a[2], w[0], low);
+    low = mfma<bf16>(a[1], w[1], low);
+    low = mfma<bf16>(a[0], w[2], low);
+    low = mfma<bf16>(a[1], w[0], low);
+    low = mfma<bf16>(a[0], w[1], low);
+    high = mfma<bf16>(a[0], w[0], high);
   }
 };
 
-// z of 32 rows of the table: four waves share the columns, 64 at a time, and add their sums through LDS.
+// Few tokens, or few rows of the table: a workgroup has z of 32 rows of the table and 32 tokens, whose parts come from L2.  Four waves share
+// the columns, 64 at a time, and add their sums through LDS.
 constexpr int kFewRows = 32;
-template <int EPI, int NB>
+template <int EPI>
 __global__ __launch_bounds__(kThreads) void kan_vocab_few_kernel(const ProductArgs g) {
   __shared__ float sSum[4][16][64];
   __shared__ float2 sStat[4][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ln = lane & 31, lh = lane >> 5;
-  const int n_here = g.count ? min(g.n, *g.count) : g.n, m0 = (int)blockIdx.x * kFewRows;
-  if (n_here == 0) return;
+  const int n_here = g.count ? min(g.n, *g.count) : g.n, m0 = (int)blockIdx.x * kFewRows, n0 = (int)blockIdx.y * 32;
+  if (n0 >= n_here) return;
   const float* const row = (const float*)g.a.p + (long long)min(m0 + ln, g.m - 1) * g.a.stride;
-  const bf16* b[NB];
-#pragma unroll
-  for (int j = 0; j < NB; ++j) b[j] = (const bf16*)g.b.p + (long long)min(32 * j + ln, n_here - 1) * g.b.stride;
-  FewSums<NB> sums;
+  const bf16* const b = (const bf16*)g.b.p + (long long)min(n0 + ln, n_here - 1) * g.b.stride;
+  FewSums sums;
   sums.clear();
   for (int k0 = wave * 64; k0 < g.k; k0 += 256) {
     float v[4][8];
@@ -539,80 +549,73 @@ __global__ __launch_bounds__(kThreads) void kan_vocab_few_kernel(const ProductAr
         }
     }
 #pragma unroll
-    for (int h = 0; h < 4; ++h) sums.add(v[h], b, k0 + 16 * h + 8 * lh, g.b.part);      // (zeros behind B's last column)
+    for (int h = 0; h < 4; ++h) sums.add(v[h], b + k0 + 16 * h + 8 * lh, g.b.part);      // (zeros behind B's last column)
   }
   const float scale = g.scale * 1.44269504088896f;
   const int m = 8 * wave + 4 * lh, rows = g.m - m0 - m;       // the lane's four rows of token ln
+  const int n = n0 + ln;
 #pragma unroll
-  for (int j = 0; j < NB; ++j) {
-    const int n = 32 * j + ln;
+  for (int i = 0; i < 16; ++i) sSum[wave][i][lane] = sums.high[i] + sums.low[i];
+  __syncthreads();
+  float z[4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sSum[wave][i][lane] = sums.high[j][i] + sums.low[j][i];
+  for (int q = 0; q < 4; ++q) z[q] = (sSum[0][4 * wave + q][lane] + sSum[1][4 * wave + q][lane]) + (sSum[2][4 * wave + q][lane] + sSum[3][4 * wave + q][lane]);
+  if constexpr (EPI == kStats) {
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      z[q] = q < rows ? z[q] * scale : -INFINITY;
+      top = fmaxf(top, z[q]);
+    }
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float at = fminf(fmaxf(top, -FLT_MAX), FLT_MAX);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum += __builtin_amdgcn_exp2f(z[q] - at);
+    sum += __shfl_xor(sum, 32);
+    if (lh == 0) sStat[wave][ln] = make_float2(at, sum);
     __syncthreads();
-    float z[4];
+    if (threadIdx.x < 32 && n < g.n) {
+      float all = sStat[0][ln].x, total = 0.f;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) z[q] = (sSum[0][4 * wave + q][lane] + sSum[1][4 * wave + q][lane]) + (sSum[2][4 * wave + q][lane] + sSum[3][4 * wave + q][lane]);
-    if constexpr (EPI == kStats) {
-      float top = -INFINITY, sum = 0.f;
+      for (int w = 1; w < 4; ++w) all = fmaxf(all, sStat[w][ln].x);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) total += sStat[w][ln].y * __builtin_amdgcn_exp2f(sStat[w][ln].x - all);
+      g.stats[(long long)((g.v0 + m0) / kFewRows) * g.n + n] = make_float2(all, total);
+    }
+  } else {
+    if (n < n_here) {
+      const float lse = g.lse[n] * 1.44269504088896f, weight = g.weight[n];
+      const int hit = (int)((uint32_t)g.targets[n] - (uint32_t)(g.v0 + m0) - (uint32_t)m);
+      float v[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        z[q] = q < rows ? z[q] * scale : -INFINITY;
-        top = fmaxf(top, z[q]);
+        const float e = __builtin_amdgcn_exp2f(fmaf(z[q], scale, -lse));
+        v[q] = q < rows ? (q == hit ? e - 1.f : e) * weight : 0.f;
       }
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float at = fminf(fmaxf(top, -FLT_MAX), FLT_MAX);
+      bf16* dst = (bf16*)g.ds + (long long)n * g.ds_stride + m0 + m;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) sum += __builtin_amdgcn_exp2f(z[q] - at);
-      sum += __shfl_xor(sum, 32);
-      if (lh == 0) sStat[wave][ln] = make_float2(at, sum);
-      __syncthreads();
-      if (threadIdx.x < 32 && n < g.n) {
-        float all = sStat[0][ln].x, total = 0.f;
-#pragma unroll
-        for (int w = 1; w < 4; ++w) all = fmaxf(all, sStat[w][ln].x);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) total += sStat[w][ln].y * __builtin_amdgcn_exp2f(sStat[w][ln].x - all);
-        g.stats[(long long)((g.v0 + m0) / kFewRows) * g.n + n] = make_float2(all, total);
-      }
-    } else {
-      if (n < n_here) {
-        const float lse = g.lse[n] * 1.44269504088896f, weight = g.weight[n];
-        const int hit = (int)((uint32_t)g.targets[n] - (uint32_t)(g.v0 + m0) - (uint32_t)m);
-        float v[4];
+      for (int p = 0; p < 3; ++p, dst += g.ds_part) {
+        typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        bf16x4 t;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const float e = __builtin_amdgcn_exp2f(fmaf(z[q], scale, -lse));
-          v[q] = q < rows ? (q == hit ? e - 1.f : e) * weight : 0.f;
+          t[q] = (bf16)v[q];
+          v[q] -= (float)t[q];
         }
-        bf16* dst = (bf16*)g.ds + n * g.ds_stride + m0 + m;
-#pragma unroll
-        for (int p = 0; p < 3; ++p, dst += g.ds_part) {
-          typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
-          bf16x4 t;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            t[q] = (bf16)v[q];
-            v[q] -= (float)t[q];
-          }
-          *(bf16x4*)dst = t;
-        }
+        *(bf16x4*)dst = t;
       }
     }
-    __syncthreads();
   }
 }
 
-// dh's slices: four waves take 32 columns each of the same rows of the table.
-template <int NB>
+// dh's slices of up to 32 tokens: four waves take 32 columns each of the same rows of the table.
 __global__ __launch_bounds__(kThreads) void kan_vocab_few_rows_kernel(const ProductArgs g) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ln = lane & 31, lh = lane >> 5;
   const int n_here = min(g.n, *g.count), d0 = (int)blockIdx.x * 128 + wave * 32, split = blockIdx.y;
   if (n_here == 0 || d0 >= g.m) return;
   const float* const column = (const float*)g.a.p + min(d0 + ln, g.m - 1);
-  const bf16* b[NB];
-#pragma unroll
-  for (int j = 0; j < NB; ++j) b[j] = (const bf16*)g.b.p + (long long)min(32 * j + ln, n_here - 1) * g.b.stride;
-  FewSums<NB> sums;
+  const bf16* const b = (const bf16*)g.b.p + (long long)min(ln, n_here - 1) * g.b.stride;
+  FewSums sums;
   sums.clear();
   const long long steps = (g.k + 31) / 32;
   const int s0 = (int)(steps * split / g.splits), s1 = (int)(steps * (split + 1) / g.splits);
@@ -623,17 +626,223 @@ __global__ __launch_bounds__(kThreads) void kan_vocab_few_rows_kernel(const Prod
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[h][i] = column[(long long)min(32 * s + 16 * h + 8 * lh + i, g.k - 1) * g.a.stride];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) sums.add(v[h], b, 32 * s + 16 * h + 8 * lh, g.b.part);       // (dS is zero behind the last row)
+    for (int h = 0; h < 2; ++h) sums.add(v[h], b + 32 * s + 16 * h + 8 * lh, g.b.part);       // (dS is zero behind the last row)
   }
+  float* const out = (float*)g.out + split * g.out_slice + ln * g.out_stride;
 #pragma unroll
-  for (int j = 0; j < NB; ++j) {
-    const int n = 32 * j + ln;
-    float* const out = (float*)g.out + split * g.out_slice + n * g.out_stride;
+  for (int i = 0; i < 16; ++i) {
+    const int d = d0 + 8 * (i >> 2) + 4 * lh + (i & 3);
+    if (ln < n_here && d < g.m) out[d] = sums.high[i] + sums.low[i] + (g.add ? out[d] : 0.f);
+  }
+}
+
+// Tiles of 32 WM rows of the table (dh: columns) and 32 CB WN tokens.  A wave has 32 of the rows as fragments straight from memory, two steps of
+// 32 ahead, and splits the next half of a step while this one is multiplied; the tokens' parts pass through LDS for all waves, a ring of three
+// steps.  One barrier a step, in front of its last six products.
+template <int CB_, int WM_>
+struct SplitShape {
+  static constexpr int RB = 1, CB = CB_, WM = WM_, WN = 4 / WM_;
+  static constexpr int BM = 32 * WM, BN = 32 * CB * WN, kHeld = (BN + 63) / 64 * 64, kSlots = 3, kLds = kSlots * 3 * kHeld * kStep * 2;
+};
+// AK: z (else dh): the contraction is over the columns of the table.
+template <bool AK, int EPI, class S>
+__device__ __forceinline__ void split_product(const ProductArgs& g, const unsigned block, unsigned char* const sRing) {
+  constexpr int CB = S::CB, BM = S::BM, BN = S::BN, kSlots = S::kSlots, kAhead = 2;
+  typedef Tile<bf16, true, S::kHeld> TB;
+  constexpr int kSlot = 3 * TB::kBytes, kCopies = 3 * TB::kCopies;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, lh = lane >> 5;
+  const int wm = wave % S::WM * 32, n_here = g.count ? min(g.n, *g.count) : g.n;
+  int mt, nt, split;
+  if (!place(block, (unsigned)(g.m + BM - 1) / BM, (unsigned)(n_here + BN - 1) / BN, (unsigned)g.splits, &mt, &nt, &split)) return;
+  const int m0 = mt * BM, n0 = nt * BN;
+  const int steps = (g.k + kStep - 1) / kStep, s0 = (int)((long long)steps * split / g.splits), s1 = (int)((long long)steps * (split + 1) / g.splits);
+  TB B;
+  B.init(g.b, n0, wave, lane, wave / S::WM * 32 * CB);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sRing;
+  // (a step past the last one: a buffer of no bytes)
+  auto copy = [&](int s, int slot) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int d = d0 + 8 * (i >> 2) + 4 * lh + (i & 3);
-      if (n < n_here && d < g.m) out[d] = sums.high[j][i] + sums.low[j][i] + (g.add ? out[d] : 0.f);
+    for (int p = 0; p < 3; ++p) {
+      B.aim((uint32_t)p, s < s1 ? g.b.depth : 0, s * kStep);
+      const u32x4 r = B.buffer();
+#pragma unroll
+      for (int j = 0; j < TB::kCopies; ++j) B.copy(r, j, wave, lds0 + (uint32_t)(slot * kSlot + p * TB::kBytes), s * kStep, g.b.depth);
     }
+  };
+  // A: rows past the last one repeat it.  Bytes from the tile's first element on.
+  const char* const a0 = (const char*)g.a.p + (AK ? (long long)m0 * g.a.stride * 4 : (long long)m0 * 4);
+  const long long row = g.a.stride * 4;
+  const uint32_t r0 = (uint32_t)(min(m0 + wm + ln, g.m - 1) - m0), ao = AK ? r0 * (uint32_t)row + lh * 32u : r0 * 4u + lh * 8u * (uint32_t)row;
+  // Half h of a step: eight numbers of k = 16 h + 8 lh on.  (Always loads, so that the compiler's waits count the same loads on every way.)
+  float a[kAhead][2][8];
+  auto fetch = [&](int s, int h, auto P) __attribute__((always_inline)) {
+    constexpr int to = decltype(P)::value;
+    const int k0 = min(s, s1 - 1) * kStep;
+    if (k0 + kStep <= g.k) {
+      if constexpr (AK) {
+        load8((const float*)(a0 + (long long)k0 * 4 + ao) + 16 * h, a[to][h]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[to][h][e] = *(const float*)(a0 + (long long)(k0 + 16 * h + e) * row + ao);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int k = k0 + 16 * h + e;
+        a[to][h][e] = k + 8 * lh < g.k ? *(const float*)(a0 + (AK ? (long long)k * 4 : (long long)k * row) + ao) : 0.f;
+      }
+      __builtin_amdgcn_s_waitcnt(0);
+    }
+  };
+  // Parts of both halves: one is multiplied while the other is formed, two numbers at a time.
+  uint32_t parts[2][3][4];
+  auto cut = [&](int h, int pair, int p, auto P) __attribute__((always_inline)) {
+    constexpr int from = decltype(P)::value;
+    parts[h][p][pair] = next_part(a[from][h][2 * pair], a[from][h][2 * pair + 1], p == 2);
+    asm volatile("" : "+v"(parts[h][p][pair]));       // (formed here, beside the products, not where it is used)
+  };
+  f32x16 high[1][CB], low[CB];
+#pragma unroll
+  for (int j = 0; j < CB; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) high[0][j][r] = low[j][r] = 0.f;
+  uint4 w[2][3];
+  int slot = 0;
+  auto read = [&](int s, int group, int to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < 3; ++p) B.fragment(sRing + s * kSlot + p * TB::kBytes, group % CB, group / CB, 0, w[to][p]);
+  };
+  // Groups of six products: half h of a block of 32 tokens.  Behind the first of them the next group's fragments are asked for, between the
+  // others the next half's parts are formed.
+  auto step = [&](int s, auto now) __attribute__((always_inline)) {
+    const std::integral_constant<int, (decltype(now)::value + 1) % kAhead> next;
+    const int last = slot >= 1 ? slot - 1 : kSlots - 1, after = slot + 1 == kSlots ? 0 : slot + 1;
+    copy(s + kSlots - 1, last);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int q = 0; q < 2 * CB; ++q) {
+      const int h = q / CB, j = q % CB;
+      if (j == 0) {
+        fetch(s + kAhead, h, now);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (q == 2 * CB - 1) {
+        // The last reads of this slot are done, and the next one is there.  Behind its copies are those of kSlots - 2 later ones, and the loads
+        // of as many steps and this one, four each at least, where the step that these are for exists (the compiler leaves out those that nothing needs).
+        if (s + kAhead < s1) copies_done<kCopies * (kSlots - 2) + 4 * (kSlots - 1)>();
+        else copies_done<kCopies * (kSlots - 2)>();
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      uint4 v[3];
+#pragma unroll
+      for (int p = 0; p < 3; ++p) v[p] = make_uint4(parts[h][p][0], parts[h][p][1], parts[h][p][2], parts[h][p][3]);
+      const uint4(&b)[3] = w[q & 1];
+      constexpr int kSmall = 5, kPartsA[] = {2, 1, 0, 1, 0}, kPartsB[] = {0, 1, 2, 0, 1};
+#pragma unroll
+      for (int m = 0; m <= kSmall; ++m) {
+        if (m < kSmall) low[j] = mfma<bf16>(v[kPartsA[m]], b[kPartsB[m]], low[j]);
+        else high[0][j] = mfma<bf16>(v[0], b[0], high[0][j]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (m == 0) read(q == 2 * CB - 1 ? after : slot, q == 2 * CB - 1 ? 0 : q + 1, (q + 1) & 1);
+        const int first = j * 12 / CB, count = (j + 1) * 12 / CB - first;
+#pragma unroll
+        for (int c = first + m * count / (kSmall + 1); c < first + (m + 1) * count / (kSmall + 1); ++c) {
+          if (h == 0) cut(1, c / 3, c % 3, now);
+          else cut(0, c / 3, c % 3, next);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    slot = after;
+  };
+  if (s0 < s1) {
+#pragma unroll
+    for (int i = 0; i < kSlots - 1; ++i) copy(s0 + i, i);
+    const std::integral_constant<int, 0> even;
+    const std::integral_constant<int, 1> odd;
+    fetch(s0, 0, even);
+    fetch(s0, 1, even);
+    fetch(s0 + 1, 0, odd);
+    fetch(s0 + 1, 1, odd);
+#pragma unroll
+    for (int c = 0; c < 12; ++c) cut(0, c / 3, c % 3, even);
+    copies_done<kCopies * (kSlots - 2)>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    read(0, 0, 0);
+    int s = s0;
+    for (; s + 2 <= s1; s += 2) {
+      step(s, even);
+      step(s + 1, odd);
+    }
+    if (s < s1) step(s, even);
+  }
+  copies_done<0>();
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < CB; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) high[0][j][r] += low[j][r];
+  finish<bf16, EPI, S>(g, high, m0, n0, split, n_here, sRing);
+}
+template <bool AK, int EPI, class S>
+__global__ __launch_bounds__(kThreads, 2) void kan_vocab_split_kernel(const ProductArgs g) {
+  __shared__ __attribute__((aligned(1024))) unsigned char sRing[S::kLds];
+  split_product<AK, EPI, S>(g, blockIdx.x, sRing);
+}
+// dh and dT of a piece in one launch, as kan_vocab_grads_kernel.
+template <class R, class S>
+__global__ __launch_bounds__(kThreads, 2) void kan_vocab_split_grads_kernel(const ProductArgs rows, const ProductArgs table, unsigned row_blocks) {
+  __shared__ __attribute__((aligned(1024))) unsigned char sRing[R::kLds > S::kLds ? R::kLds : S::kLds];
+  if (blockIdx.x < row_blocks) split_product<false, kGradRows, R>(rows, blockIdx.x, sRing);
+  else product<bf16, false, false, kGradTable, S>(table, blockIdx.x - row_blocks, sRing);
+}
+
+// z from its slices [slice][token][row] (few tiles: shares of the columns each): a wave has 256 rows of the table and a token.
+constexpr int kSumRows = 256;
+template <int EPI>
+__global__ __launch_bounds__(kThreads) void kan_vocab_sums_kernel(const ProductArgs g, const float* __restrict__ src, int slices, unsigned chunks) {
+  const int lane = threadIdx.x & 63, n = (int)(blockIdx.x / chunks) * 4 + (threadIdx.x >> 6), n_here = g.count ? min(g.n, *g.count) : g.n;
+  if (n >= n_here) return;
+  const unsigned chunk = blockIdx.x % chunks;
+  const int m = (int)chunk * kSumRows + lane * 4, rows = g.m - m;
+  float z[4] = {0.f, 0.f, 0.f, 0.f};
+  if (rows > 0) {
+#pragma unroll 4
+    for (int k = 0; k < slices; ++k) {
+      const float4 t = *(const float4*)(src + k * g.out_slice + n * g.out_stride + m);       // (rows of whole float4)
+      z[0] += t.x, z[1] += t.y, z[2] += t.z, z[3] += t.w;
+    }
+  }
+  const float scale = g.scale * 1.44269504088896f;
+  if constexpr (EPI == kStats) {
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      z[q] = q < rows ? z[q] * scale : -INFINITY;
+      top = fmaxf(top, z[q]);
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float at = fminf(fmaxf(top, -FLT_MAX), FLT_MAX);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum += __builtin_amdgcn_exp2f(z[q] - at);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+    if (lane == 0) g.stats[((long long)(g.v0 / kSumRows) + chunk) * g.n + n] = make_float2(at, sum);
+  } else {
+    const float lse = g.lse[n] * 1.44269504088896f, weight = g.weight[n];
+    const int hit = (int)((uint32_t)g.targets[n] - (uint32_t)g.v0 - (uint32_t)m);
+    float v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float e = __builtin_amdgcn_exp2f(fmaf(z[q], scale, -lse));
+      v[q] = q < rows ? (q == hit ? e - 1.f : e) * weight : 0.f;
+    }
+    uint2* dst = (uint2*)((bf16*)g.ds + (long long)n * g.ds_stride + m);
+#pragma unroll
+    for (int p = 0; p < 3; ++p, dst = (uint2*)((bf16*)dst + g.ds_part)) *dst = make_uint2(next_part(v[0], v[1]), next_part(v[2], v[3]));
   }
 }
 
@@ -971,16 +1180,18 @@ int pick_tiles(long long m, long long n, long long steps, bool stats) {
   return best;
 }
 
-// dh and dT of a piece of V rows: tiles of both, and the shares in which dh's long contraction is done where it has few tiles:
-// each adds a slice of N x D sums that is written and read once.
-void pick_grads(long long N, long long V, long long D, int parts, int* kind, int* slices) {
+// dh and dT of a piece of V rows, which share a launch: tiles of both (from `first` on), and the shares in which dh's long contraction is done where it
+// has few tiles: each adds a slice of N x D sums that is written and read once.  At most `most` workgroups fit a CU; row_ns(kind, steps, on), row_tiles(kind):
+// ns of a tile of dh, and how many.  Returns ns.
+template <class Ns, class Tiles>
+long long pick_shares(long long N, long long V, long long D, int parts, int first, long long most, long long steps, Ns&& row_ns, Tiles&& row_tiles, int* kind, int* slices) {
   long long least = -1;
-  const long long steps = steps_of(V, parts), table_steps = steps_of(N, parts);
-  for (int k = 0; k < kTileKinds; ++k)
+  const long long table_steps = steps_of(N, parts);
+  for (int k = first; k < kTileKinds; ++k)
     for (int s = 1; s <= 32 && (s == 1 || steps / s >= 8); ++s) {
-      const long long n1 = tiles_of(k, D, N) * s, n2 = tiles_of(k, D, V), slots = kCus * kPerCu[k], row_steps = (steps + s - 1) / s;
-      const long long on = std::min(kPerCu[k], (n1 + n2 + kCus - 1) / kCus);
-      const long long rows = tile_ns(k, row_steps, false, on), table = tile_ns(k, table_steps, false, on);
+      const long long n1 = row_tiles(k) * s, n2 = tiles_of(k, D, V), per = std::min(most, kPerCu[k]), slots = kCus * per, row_steps = (steps + s - 1) / s;
+      const long long on = std::min(per, (n1 + n2 + kCus - 1) / kCus);
+      const long long rows = row_ns(k, row_steps, on), table = tile_ns(k, table_steps, false, on);
       // the longest, if all have a place at once; else dh's rounds, or the CUs' work in all and the end of the last tiles, dT's
       long long c = std::max(rows, table);
       if (n1 + n2 > slots) c = std::max((n1 + slots - 1) / slots * rows, (n1 * rows + n2 * table) / slots + tile_ns(k, table_steps, false, 1) / 2);
@@ -991,6 +1202,11 @@ void pick_grads(long long N, long long V, long long D, int parts, int* kind, int
         *slices = s;
       }
     }
+  return least;
+}
+void pick_grads(long long N, long long V, long long D, int* kind, int* slices) {
+  pick_shares(N, V, D, 1, 0, 3, steps_of(V, 1), [](int k, long long steps, long long on) { return tile_ns(k, steps, false, on); },
+              [&](int k) { return tiles_of(k, D, N); }, kind, slices);
 }
 
 // f(S{}) for the shape of a kind.
@@ -1021,68 +1237,158 @@ hipError_t launch_grads(const ProductArgs& rows, const ProductArgs& table, int k
   });
 }
 
-// f(NB{}) for the blocks of 32 of n tokens.
-constexpr int kFewTokens = 64;
-template <class F>
-hipError_t with_blocks(long long n, F&& f) {
-  if (n <= 32) return f(std::integral_constant<int, 1>{});
-  return f(std::integral_constant<int, 2>{});
-}
 template <int EPI>
 hipError_t launch_few(const ProductArgs& g, hipStream_t s) {
-  return with_blocks(g.n, [&](auto nb) {
-    hipLaunchKernelGGL((kan_vocab_few_kernel<EPI, decltype(nb)::value>), dim3((unsigned)(g.m + kFewRows - 1) / kFewRows), dim3(kThreads), 0, s, g);
-    return hipGetLastError();
-  });
+  hipLaunchKernelGGL((kan_vocab_few_kernel<EPI>), dim3((unsigned)(g.m + kFewRows - 1) / kFewRows, (unsigned)(g.n + 31) / 32), dim3(kThreads), 0, s, g);
+  return hipGetLastError();
 }
 hipError_t launch_few_rows(const ProductArgs& g, hipStream_t s) {
-  return with_blocks(g.n, [&](auto nb) {
-    hipLaunchKernelGGL((kan_vocab_few_rows_kernel<decltype(nb)::value>), dim3((unsigned)(g.m + 127) / 128, (unsigned)g.splits), dim3(kThreads), 0, s, g);
+  hipLaunchKernelGGL(kan_vocab_few_rows_kernel, dim3((unsigned)(g.m + 127) / 128, (unsigned)g.splits), dim3(kThreads), 0, s, g);
+  return hipGetLastError();
+}
+
+// fp32: tiles of kan_vocab_split_kernel, and the kernels for few (z: kSplitKinds stands for kan_vocab_few_kernel).
+enum SplitKind : int { k128x32, k128x64s, k128x96, k128x128, k64x128, kSplitKinds };
+constexpr int kSplitM[] = {128, 128, 128, 128, 64}, kSplitN[] = {32, 64, 96, 128, 128};
+// ns of a step of 32 with one and two workgroups on a CU (measured on products of 30,000 x 4,000, 94,000 x 1,530, 13,000 x 1,700 and 5,000 x 3,500 with 1
+// to 400 tokens; beyond about 2,300 it is the matrix cores and their power).
+constexpr long long kSplitAlone[] = {1100, 1150, 1250, 1350, 1000}, kSplitFull[] = {2000, 2200, 2500, 2600, 2000};
+long long split_tiles(int kind, long long m, long long n) { return ((m + kSplitM[kind] - 1) / kSplitM[kind]) * ((n + kSplitN[kind] - 1) / kSplitN[kind]); }
+// z of m rows of the table and n tokens.  Few: every column takes a workgroup 10 ns, and the GPU 30 to 50 ps (the more of its 32 tokens exist the more
+// cache lines of these it reads).  Loss in us, few and split: 1 x 94,000 x 1,530 141 and 171, 32 x 94,000 x 1,530 248 and 194, 32 x 1,300 x 4,000 47 and 99,
+// 64 x 13,000 x 1,700 74 and 58, 200 x 2,000 x 1,024 31 and 43, 400 x 2,000 x 1,024 48 and 44.  Tiles that leave CUs idle: shares of the columns, whose sums are
+// written, read and added (500 x 1,300 x 4,000 whole 146, in shares 56, 128 x 5,000 x 3,500 108 and 49).
+int pick_split(long long m, long long n, long long D, int* slices) {
+  const long long groups = (m + kFewRows - 1) / kFewRows * ((n + 31) / 32), steps = (D + kStep - 1) / kStep;
+  int best = kSplitKinds;
+  long long least = n > 1 << 20 ? INT64_MAX : D * std::max(10000ll, groups * (30 + 6 * std::min(n, 32ll) / 10)) / 1000;      // (65,536 blocks of tokens a launch)
+  *slices = 1;
+  for (int kind = 0; kind < kSplitKinds; ++kind)
+    for (int s = 1; s <= 16 && (s == 1 || steps / s >= 8); ++s) {
+      const long long tiles = split_tiles(kind, m, n) * s, rest = tiles % (2 * kCus);
+      if (s > 1 && tiles > 2 * kCus) break;
+      const long long c = (steps + s - 1) / s * (tiles / (2 * kCus) * kSplitFull[kind] + (rest > kCus ? kSplitFull[kind] : rest ? kSplitAlone[kind] : 0)) +
+                          (s == 1 ? 0 : 6000 + m * n * 8 * s / 4000);
+      if (c < least) {
+        least = c;
+        best = kind;
+        *slices = s;
+      }
+    }
+  return best;
+}
+
+template <bool AK, int EPI>
+hipError_t launch_split(const ProductArgs& g, int kind, hipStream_t s) {
+  auto launch = [&](auto shape) {
+    hipLaunchKernelGGL((kan_vocab_split_kernel<AK, EPI, decltype(shape)>), dim3((unsigned)(split_tiles(kind, g.m, g.n) * g.splits)), dim3(kThreads), 0, s, g);
     return hipGetLastError();
-  });
+  };
+  if (kind == k128x32) return launch(SplitShape<1, 4>{});
+  if (kind == k128x64s) return launch(SplitShape<2, 4>{});
+  if (kind == k128x96) return launch(SplitShape<3, 4>{});
+  if constexpr (AK)
+    if (kind == k64x128) return launch(SplitShape<2, 2>{});
+  return launch(SplitShape<4, 4>{});
+}
+hipError_t launch_split_grads(const ProductArgs& rows, const ProductArgs& table, int kind, hipStream_t s) {
+  const unsigned row_blocks = (unsigned)((split_tiles(k128x128, rows.m, rows.n) * rows.splits + 7) / 8 * 8);
+  auto launch = [&](auto shape) {
+    hipLaunchKernelGGL((kan_vocab_split_grads_kernel<SplitShape<4, 4>, decltype(shape)>), dim3(row_blocks + (unsigned)tiles_of(kind, table.m, table.n)), dim3(kThreads), 0, s,
+                       rows, table, row_blocks);
+    return hipGetLastError();
+  };
+  if (kind == k256x128) return launch(Shape<4, 2, 2, 2, 3>{});
+  if (kind == k256x64) return launch(Shape<2, 2, 4, 1, 4>{});
+  return launch(Shape<2, 1, 2, 2, 4>{});
+}
+// z, in slices or at once, and what becomes of it.
+template <int EPI>
+hipError_t launch_fp32(const ProductArgs& g, int kind, int slices, float* sums, hipStream_t s) {
+  if (kind == kSplitKinds) return launch_few<EPI>(g, s);
+  if (slices == 1) return launch_split<true, EPI>(g, kind, s);
+  ProductArgs z = g;
+  z.splits = slices;
+  z.out = sums;
+  z.out_stride = (g.m + 3) / 4 * 4;
+  z.out_slice = z.out_stride * g.n;
+  z.out_dtype = KAN_F32;
+  const hipError_t e = launch_split<true, kGradRows>(z, kind, s);
+  if (e != hipSuccess) return e;
+  const unsigned chunks = (unsigned)(g.m + kSumRows - 1) / kSumRows;
+  hipLaunchKernelGGL((kan_vocab_sums_kernel<EPI>), dim3(chunks * ((unsigned)(g.n + 3) / 4)), dim3(kThreads), 0, s, z, (const float*)sums, slices, chunks);
+  return hipGetLastError();
 }
 
 struct Plan {
   int parts;
-  bool few;                   // fp32 tokens that do not make it worth to write the table's parts
   bool pack_table, pack_rows; // the table's rows, h go through the workspace
   long long width;            // columns of packed rows
   int piece, pieces;          // rows of the table that are dealt with at a time
-  int slices;                 // of dh
-  int z_kind, grad_kind;      // tiles of z, of dh and dT (few: of dT)
+  int slices, z_slices;       // of dh; fp32: of z
+  int z_kind, rows_kind;      // tiles of z, of dh (fp32: SplitKind, kSplitKinds for few; else dh has dT's)
+  int grad_kind;              // tiles of dT
+  bool together;              // fp32: dh and dT in one launch
   int stat_rows;              // of the table that share statistics
-  size_t h, table, stats, list, target, lse, weight, scalars, ds, dh, bytes;
+  size_t h, table, sums, stats, list, target, lse, weight, scalars, ds, dh, bytes;
 };
 
 Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
   Plan p = {};
-  p.parts = dtype == KAN_F32 ? 3 : 1;
-  p.few = dtype == KAN_F32 && N <= kFewTokens;
-  p.pack_table = !p.few && (p.parts > 1 || D % 8 != 0);
-  p.pack_rows = p.few || p.pack_table;
+  const bool fp32 = dtype == KAN_F32;
+  p.parts = fp32 ? 3 : 1;
+  p.pack_table = !fp32 && D % 8 != 0;
+  p.pack_rows = fp32 || p.pack_table;
   p.width = ((long long)D + 63) / 64 * 64;
   const long long all = ((long long)V + kVocabStep - 1) / kVocabStep * kVocabStep;
   long long piece = all;
   auto limit = [&](long long budget, long long row_bytes) { piece = std::min(piece, std::max(1ll, budget / (row_bytes * kVocabStep)) * kVocabStep); };
-  // Packed pieces that the memory-side cache holds (426 x 36,161 x 2,235 in fp32 2,170 us, in one piece 2,390), but not fewer rows than
-  // give the CUs three tiles of 128 x 64 each, while that is 2 GiB or less (128 x 30,000 x 2,048 838 us for 1,075; 70 x 100,000 x 1,024 1,476 for 1,421).
-  if (p.pack_table) limit(std::max(kPackBytes, std::min(2ll << 30, 3ll * kCus * 128 / ((N + 63) / 64) * p.parts * p.width * 2)), p.parts * p.width * 2);
-  // (fewer than 2^24 workgroups a launch, whose threads have 32 bits: tiles of 128 x 64, few: 32 rows)
+  // Packed pieces that the memory-side cache holds.
+  if (p.pack_table) limit(kPackBytes, p.width * 2);
+  // (fewer than 2^24 workgroups a launch, whose threads have 32 bits: tiles of 128 x 64, fp32: 32 rows)
   limit(1ll << 36, N);
-  limit(p.few ? 1ll << 28 : 1ll << 30, 1);
+  limit(fp32 ? 1ll << 28 : 1ll << 30, 1);
   if (backward) {
-    limit(kPieceBytes, p.parts * N * 2);
+    limit(kPieceBytes, N * 2);      // (of a part)
     limit(1ll << 35, D);
     limit(1ll << 25, 1);           // (32 rows of dS: 32-bit offsets)
   }
-  p.piece = (int)std::min(piece, (long long)INT32_MAX / kVocabStep * kVocabStep);
-  p.pieces = (int)((V + (long long)p.piece - 1) / p.piece);
-  p.z_kind = pick_tiles(std::min(p.piece, V), N, steps_of(D, p.parts), !backward);
-  p.stat_rows = p.few ? kFewRows : kTileM[p.z_kind];
-  if (backward) pick_grads(N, std::min(p.piece, V), D, p.parts, &p.grad_kind, &p.slices);
-  if (p.few) {       // four workgroups a CU (two blocks of tokens: two, 64 x 30,000 x 1,024 296 against 317 us), with 64 rows of the table each or more
-    p.grad_kind = pick_tiles(D, std::min(p.piece, V), steps_of(N, p.parts), false);
-    p.slices = (int)std::max(1ll, std::min({256ll, (N > 32 ? 2ll : 4ll) * kCus / ((D + 127) / 128), (long long)std::min(p.piece, V) / 64}));
+  p.pieces = (int)((all + piece - 1) / piece);
+  p.piece = (int)((all / kVocabStep + p.pieces - 1) / p.pieces * kVocabStep);       // (of one size)
+  p.pieces = (int)((all + p.piece - 1) / p.piece);
+  const long long rows = std::min(p.piece, V);
+  if (fp32) {
+    p.z_kind = pick_split(rows, N, D, &p.z_slices);
+    p.stat_rows = p.z_kind == kSplitKinds ? kFewRows : p.z_slices > 1 ? kSumRows : kSplitM[p.z_kind];
+  } else {
+    p.z_kind = pick_tiles(rows, N, steps_of(D, 1), !backward);
+    p.stat_rows = kTileM[p.z_kind];
+  }
+  if (backward && fp32) {
+    // dh: the fewest blocks of 32 tokens, two workgroups a CU (four: 2 to 4 % longer, one: up to 20 %), slices of 256 rows of the table or more.  Narrow rows of up
+    // to 32 tokens: four a CU, 64 rows or more (32 x 1,000 x 256 39 us for 44).
+    p.grad_kind = pick_tiles(D, rows, steps_of(N, 3), false);
+    if (N <= 32 && D <= 256) {
+      p.rows_kind = kSplitKinds;
+      p.slices = (int)std::max(1ll, std::min({256ll, 4ll * kCus / ((D + 127) / 128), rows / 64}));
+    } else {
+      p.rows_kind = N <= 32 ? k128x32 : N <= 64 ? k128x64s : (N + 95) / 96 * 3 < (N + 127) / 128 * 4 ? k128x96 : k128x128;
+      p.slices = (int)std::max(1ll, std::min({128ll, 2ll * kCus / split_tiles(p.rows_kind, D, N), rows / 256}));
+    }
+    if (p.rows_kind == k128x128) {       // or with dT, if that is done before both launches are
+      const long long tiles = split_tiles(k128x128, D, N), steps = (rows + kStep - 1) / kStep, n = tiles * p.slices;
+      auto ns = [](int, long long steps, long long on) { return steps * (on > 1 ? kSplitFull[k128x128] : kSplitAlone[k128x128]) + 8000; };
+      const long long apart = (n + 2 * kCus - 1) / (2 * kCus) * ns(0, steps / p.slices, n > kCus ? 2 : 1) + N * D * 8 * (p.slices - 1) / 4000 + 3000 +
+                              rounds_ns(p.grad_kind, tiles_of(p.grad_kind, D, rows), steps_of(N, 3), false);
+      int kind, slices;
+      p.together = pick_shares(N, rows, D, 3, k256x128, 2, steps, ns, [=](int) { return tiles; }, &kind, &slices) < apart;
+      if (p.together) {
+        p.grad_kind = kind;
+        p.slices = slices;
+      }
+    }
+  } else if (backward) {
+    pick_grads(N, rows, D, &p.grad_kind, &p.slices);
   }
   size_t at = 0;
   auto take = [&](long long bytes) {
@@ -1091,7 +1397,8 @@ Plan make_plan(long long N, int V, int D, int dtype, bool backward) {
     return was;
   };
   p.h = take(backward || p.pack_rows ? p.parts * N * p.width * 2 : 0);
-  p.table = take(p.pack_table ? p.parts * (long long)p.piece * p.width * 2 : 0);
+  p.table = take(p.pack_table ? (long long)p.piece * p.width * 2 : 0);
+  p.sums = take(p.z_slices > 1 ? p.z_slices * N * (long long)p.piece * 4 : 0);
   if (!backward) {
     p.stats = take(all / p.stat_rows * N * 8);
   } else {
@@ -1174,7 +1481,7 @@ kan_status run_vocab_loss(const VocabArgs& a, hipStream_t s) {
         const PackArgs rows = {a.h, ws + p.h, i == 0 ? a.N : 0};
         if ((st = pack(job, rows, a.D, p.width, a.dtype, s)) != KAN_OK) return st;
       }
-      st = run_named("kan_vocab_loss", s, [&] { return p.few ? launch_few<kStats>(g, s) : launch_product<T, kStats>(g, p.z_kind, s); });
+      st = run_named("kan_vocab_loss", s, [&] { return p.parts == 3 ? launch_fp32<kStats>(g, p.z_kind, p.z_slices, (float*)(ws + p.sums), s) : launch_product<T, kStats>(g, p.z_kind, s); });
       if (st != KAN_OK) return st;
     }
     return run_named("kan_vocab_join", s, [&] {
@@ -1246,7 +1553,7 @@ kan_status run_vocab_grad(const VocabArgs& a, hipStream_t s) {
       g.k = a.D;
       g.a = table;
       g.b = h;
-      st = run_named("kan_vocab_ds", s, [&] { return p.few ? launch_few<kGradS>(g, s) : launch_product<T, kGradS>(g, p.z_kind, s); });
+      st = run_named("kan_vocab_ds", s, [&] { return p.parts == 3 ? launch_fp32<kGradS>(g, p.z_kind, p.z_slices, (float*)(ws + p.sums), s) : launch_product<T, kGradS>(g, p.z_kind, s); });
       if (st != KAN_OK) return st;
       // dh (+)= dS T: k = rows of the piece
       ProductArgs r = g;
@@ -1271,11 +1578,12 @@ kan_status run_vocab_grad(const VocabArgs& a, hipStream_t s) {
       g.out_dtype = a.dtype;
       g.add = a.accumulate;
       g.factor = x.factor;
-      if (p.few) {
-        if ((st = run_named("kan_vocab_rows", s, [&] { return launch_few_rows(r, s); })) != KAN_OK) return st;
+      if (p.parts == 3 && !p.together) {
+        st = run_named("kan_vocab_rows", s, [&] { return p.rows_kind == kSplitKinds ? launch_few_rows(r, s) : launch_split<false, kGradRows>(r, p.rows_kind, s); });
+        if (st != KAN_OK) return st;
         r.m = 0;            // (then there are no tiles of it)
       }
-      st = run_named("kan_vocab_grads", s, [&] { return launch_grads<T>(r, g, p.grad_kind, s); });
+      st = run_named("kan_vocab_grads", s, [&] { return p.together ? launch_split_grads(r, g, p.grad_kind, s) : launch_grads<T>(r, g, p.grad_kind, s); });
       if (st != KAN_OK) return st;
     }
     return run_named("kan_vocab_round", s, [&] {

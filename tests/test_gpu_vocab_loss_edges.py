@@ -2,6 +2,7 @@
 in 64 bits."""
 import pytest
 
+from test_gpu_vocab_loss import check_all, draw
 from tokens_testlib import HALF, check
 
 pytestmark = pytest.mark.gpu
@@ -58,3 +59,53 @@ def test_a_table_of_all_rows_that_32_bits_count(kb, dtype):
     dt[special] = want
     low, high = (float(x) for x in dt.aminmax())
     assert want - limit <= low and high <= want + limit, (low, high, want, limit)
+
+
+# few tokens over few and many rows, one to many blocks of 32 tokens; columns that end within, with and behind a step of 32; rows and tokens that end within a
+# tile of every size; a contraction over the rows in one share and many
+FULL_PRECISION = [
+    (1, 90001, 33), (3, 40000, 300), (20, 30000, 500), (32, 30011, 257), (33, 70001, 31), (50, 20011, 300), (64, 40003, 96), (65, 30000, 1), (90, 30011, 200),
+    (96, 5003, 700), (97, 30011, 95), (128, 30011, 200), (128, 10011, 333), (130, 9000, 1001), (190, 40001, 64), (200, 2000, 1024), (257, 16001, 130),
+    (280, 20001, 100), (400, 1300, 260), (400, 30003, 77), (1000, 7001, 190), (1537, 12001, 161), (7, 1003, 1999), (40, 2005, 2101), (128, 5003, 1111),
+    (500, 1300, 2000), (1000, 1001, 515),
+]
+
+
+@pytest.mark.parametrize("N,V,D", FULL_PRECISION)
+def test_tables_split_in_registers(kb, N, V, D):
+    check_all(kb, *draw(N + V + D, N, V, D, F32, ("i64", "i32")[N % 2]), scale=(1.0, 0.5)[D % 2])
+
+
+@pytest.mark.parametrize("N,V,D", [(40, 20011, 300), (200, 30011, 161)])
+def test_full_precision_rows_that_start_anywhere(kb, N, V, D):
+    """A table and rows one element behind a boundary of 16 bytes, the table's neighbours no numbers: the same bits as on their own."""
+    h, table, t, dloss = draw(3, N, V, D, F32)
+    loss, lse = kb.kan_vocab_loss_forward(h, table, t)
+    dh, dt = kb.kan_vocab_loss_backward(h, table, t, lse, dloss)
+
+    def between(a):
+        whole = torch.full((a.numel() + 33,), float("nan"), device="cuda")
+        return whole[17:17 + a.numel()].view(a.shape).copy_(a)
+    h2, table2 = between(h), between(table)
+    loss2, lse2 = kb.kan_vocab_loss_forward(h2, table2, t)
+    dh2, dt2 = kb.kan_vocab_loss_backward(h2, table2, t, lse2, dloss)
+    assert torch.equal(loss, loss2) and torch.equal(lse, lse2) and torch.equal(dh, dh2) and torch.equal(dt, dt2)
+
+
+def test_full_precision_infinite_rows_stay_in_their_tokens(kb):
+    """A row of h that is no number spoils its token; the columns behind a table's row belong to the next one and have no part in it."""
+    N, V, D = 100, 30011, 75
+    h, table, t, dloss = draw(9, N, V, D, F32, left_out=0.0)
+    clean = kb.kan_vocab_loss_forward(h, table, t)
+    h[3, 7] = float("nan")
+    loss, lse = kb.kan_vocab_loss_forward(h, table, t)
+    keep = torch.arange(N, device="cuda") != 3
+    assert bool(lse[3].isnan()) and torch.equal(loss[keep], clean[0][keep]) and torch.equal(lse[keep], clean[1][keep])
+    dl = torch.where(keep, dloss, 0.0)
+    dh, _ = kb.kan_vocab_loss_backward(torch.where(keep[:, None], h, 0.0), table, t, clean[1], dl)
+    spoiled = table.clone()
+    spoiled[V - 1] = float("inf")                   # (no target: its logits are infinite or not numbers in the last row's place alone)
+    z_last = kb.kan_vocab_loss_forward(torch.zeros_like(h), table, t)[1]
+    assert bool(torch.isfinite(z_last).all()) and bool(torch.isfinite(dh).all())
+    lse_bad = kb.kan_vocab_loss_forward(torch.where(keep[:, None], h, 0.0), spoiled, t)[1]
+    assert not bool(torch.isfinite(lse_bad[keep]).any())
