@@ -388,7 +388,10 @@ kan_status kan_vocab_loss_forward(const void* h, const void* table, int32_t dtyp
  *   g[n][v] = scale * dloss[n] * (exp(z[n][v] - lse[n]) - [v == targets[n]]),   dh = g table,   dtable = g^t h
  * dh [N][D], dtable [V][D] in `dtype`; accumulate 1: added onto what dtable holds (a table that is looked up as well).  A row
  * whose target names no row has no gradient and no part in dtable, whatever h, lse and dloss hold there.  The table is dealt
- * with in pieces, of which the workspace holds g.  dh and dtable must not overlap h or table.                                */
+ * with in pieces, of which the workspace holds g: 256 MiB, or 512 bytes a token where that is more; for KAN_F32 three times that.
+ * Between the products g is rounded to `dtype` (KAN_F32: to three bf16 numbers, 24 bits), in units of the largest |dloss|; KAN_F16
+ * keeps all its bits down to 2^-28 of that and nothing below 2^-39, so that a row whose dloss is 10^-6 of the largest has few bits
+ * of its small probabilities in dh.  dh and dtable must not overlap h or table.                                              */
 kan_status kan_vocab_loss_backward(const void* h, const void* table, int32_t dtype, int64_t N, int32_t V, int32_t D,
                                    const void* targets, int32_t id_dtype, float scale, const float* lse, const float* dloss,
                                    void* dh, void* dtable, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);

@@ -10,9 +10,11 @@
 //
 // Bound by the bytes of the rows: each is read once, a row stays in the registers of one to sixteen waves, eight columns a
 // lane at a time (8192 rows of 2048 in bf16 with fp32 blocks and gates forward 49 us, 5.4 TB/s; of 4096 in bf16 backward 111 us,
-// 4.8 TB/s; a large copy reaches 5.1).  Norms, means and the sums of the weights' gradients are fp32.  The u of the forward pass is formed from
-// the fp32 y, not from its rounded copy.  Backward: up to 512 groups of waves take rows in turn and keep the sums of their
-// rows' weight gradients in registers; a second launch adds the groups' sums in a fixed order.
+// 4.8 TB/s; a large copy reaches 5.1).  Norms, means and the sums of the weights' gradients are fp32; means are sums times a rounded 1 / D,
+// roots and sigma the hardware's (exact division and roots left the same errors, of 7e-8 to 1.2e-7 in fp32).  The u of the forward pass is
+// formed from the fp32 y, not from its rounded copy.  Backward: up to 512 groups of waves (2,048 for up to 512 columns) take rows in turn and keep
+// the sums of their rows' weight gradients; a second launch adds the groups' sums in a fixed order.  Where a lane has sixteen columns
+// (backward: widths that are no multiple of eight above 4,089, all above 8,192) some of that lies in scratch memory.
 #include <algorithm>
 #include <type_traits>
 
@@ -211,7 +213,7 @@ struct Raw {
   __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
 };
 
-// W waves a row, weights and their sums in registers: 128 of them where a lane has one group of columns, so that two rows
+// W waves a row, weights and their sums in registers (P == 1): 128 of them where widths are multiples of eight, so that two rows
 // share a CU and the loads of one run beside the sums of the other (8192 rows of 4096 in bf16: 111 us; the next row fetched
 // ahead, with 155 registers and one row a CU, 122).
 template <class S, class B, int W, int P, bool WHOLE>

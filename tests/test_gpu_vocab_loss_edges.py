@@ -109,3 +109,13 @@ def test_full_precision_infinite_rows_stay_in_their_tokens(kb):
     assert bool(torch.isfinite(z_last).all()) and bool(torch.isfinite(dh).all())
     lse_bad = kb.kan_vocab_loss_forward(torch.where(keep[:, None], h, 0.0), spoiled, t)[1]
     assert not bool(torch.isfinite(lse_bad[keep]).any())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("N", [90, 4100])
+def test_weights_far_apart(kb, N, dtype):
+    """Weights over seven orders of magnitude: an entry of fp16 g is off by 2^-39 of the largest weight beside its own rounding, of the other types by
+    its rounding alone (the bounds of Loss.grads)."""
+    h, table, t, dloss = draw(33, N, 3001, 64, dtype)
+    spread = torch.rand(N, generator=torch.Generator(device="cuda").manual_seed(5), device="cuda") * -7
+    check_all(kb, h, table, t, dloss.sign() * 10 ** (spread + 1), scale=1.0)
